@@ -413,6 +413,179 @@ int qtea_gemv_m1_static_status(int clear, qtea_stream_t stream);
  */
 int qtea_probe_decode_rates(double* cycles_per_instruction, int n);
 
+/* ======================================================================================
+ * Operators around the GEMVs of a decoder layer (not steps of the paper's method): the paged
+ * key/value cache, the attention over it, and the norms before and after a block. They take the
+ * GEMVs' fp32 outputs and give the GEMVs' fp16 inputs; PyTorch or any other owner of device
+ * memory holds every array. All are asynchronous on `stream` and allocate no device memory.
+ * ====================================================================================== */
+
+/* Element types of the arrays that may have either. */
+typedef enum qtea_type { QTEA_TYPE_F32 = 0, QTEA_TYPE_F16 = 1 } qtea_type;
+
+/*
+ * Formats of a cached row (one token's key or value of one head, head_dim elements).
+ * The quantised formats hold codes and one power of two 2^e per 32 consecutive elements, as the
+ * byte e + 127: the smallest e >= -14 with the block's largest magnitude at most 448 * 2^e (FP8)
+ * or 6 * 2^e (FP4); e = -14 for a block of zeros. Codes are x * 2^-e rounded to nearest, ties to
+ * even. Every value they stand for is exact in fp16.
+ */
+typedef enum qtea_kv_format {
+  QTEA_KV_F16 = 0, /* fp16 */
+  QTEA_KV_FP8 = 1, /* E4M3 codes, one byte each; e <= 7, magnitudes above 57344 saturate */
+  QTEA_KV_FP4 = 2  /* E2M1 codes, two per byte, the lower element in the low four bits; e <= 13,
+                      magnitudes above 49152 saturate */
+} qtea_kv_format;
+
+typedef struct qtea_kv qtea_kv; /* opaque: a paged cache in the caller's memory */
+
+/*
+ * Describe a paged key/value cache (host only; the handle borrows the caller's arrays).
+ *   k_pages, v_pages    device [n_pages][n_kv_heads][page_size][head_dim] in the format's elements
+ *                       (fp16, one byte, or half a byte each), 16-byte aligned
+ *   k_scales, v_scales  device uint8 [n_pages][n_kv_heads][page_size][head_dim / 32], 16-byte
+ *                       aligned; NULL for QTEA_KV_F16
+ *   page_size           16, 32, 64, 128 or 256 tokens;  head_dim  64 or 128
+ *   n_pages >= 1, n_kv_heads 1..1024, n_pages * n_kv_heads * page_size < 2^31
+ * A page holds the same page_size consecutive tokens of one sequence for every head. The memory
+ * may hold anything: rows that no sequence has written yet are never part of a result.
+ * Returns QTEA_OK, QTEA_ERR_INVALID_ARG, QTEA_ERR_UNSUPPORTED (another page_size or head_dim),
+ * QTEA_ERR_ALLOC (host memory) or QTEA_ERR_CUDA (no driver, or it rejects the arrays).
+ */
+int qtea_kv_create(void* k_pages, void* v_pages, void* k_scales, void* v_scales, int n_pages, int page_size,
+                   int n_kv_heads, int head_dim, int format, qtea_kv** out);
+
+/* Release the handle (not the caller's arrays). NULL is ignored. */
+void qtea_kv_free(qtea_kv* kv);
+
+/*
+ * The sequences of one call. Sequence s has ctx_len[s] tokens, of which the last
+ * q_start[s+1] - q_start[s] are new; they are rows q_start[s].. of the call's arrays, and the i-th
+ * has the position ctx_len[s] - (q_start[s+1] - q_start[s]) + i. Token p of sequence s lies in page
+ * pages[s][p / page_size], at p % page_size.
+ *   q_start  device int32 [n_seqs + 1], ascending;  ctx_len  device int32 [n_seqs]
+ *   pages    device int32 [n_seqs][max_pages]; entries past a sequence's last page are not used
+ *   n_tokens    rows of the call's arrays; rows in no sequence are neither read nor written
+ *   max_q_len   no sequence has more new tokens than this (it chooses the kernel and sizes the
+ *               workspace; the tokens of a longer sequence past it are skipped)
+ * Lengths are read on the device, so a captured graph can be replayed with others. They are
+ * bounded there: a context longer than max_pages * page_size counts as that long, a negative one
+ * as empty, and page numbers outside [0, n_pages) are never followed out of the cache.
+ * Limits: 1 <= n_seqs <= 1024 (n_seqs = 0: nothing to do), n_tokens >= 0, max_q_len >= 1, max_pages >= 1,
+ * max_pages * page_size < 2^31.
+ */
+typedef struct qtea_kv_batch {
+  const int32_t* q_start;
+  const int32_t* ctx_len;
+  const int32_t* pages;
+  int n_seqs, max_pages, n_tokens, max_q_len;
+} qtea_kv_batch;
+
+/*
+ * Arguments of qtea_kv_append. Row t of q, k, v begins at element t * ld and holds the heads one
+ * after the other (n * head_dim elements); the three may be parts of one array.
+ */
+typedef struct qtea_kv_append_args {
+  const void* q;           /* [n_tokens][n_q_heads * head_dim], or NULL: k and v alone */
+  const void* k;           /* [n_tokens][n_kv_heads * head_dim] */
+  const void* v;
+  long long q_ld, k_ld, v_ld; /* elements from one row to the next */
+  int type;                /* QTEA_TYPE_F32 (as the GEMVs write) or QTEA_TYPE_F16 */
+  int n_q_heads;
+  const float* cos;        /* [n_positions][head_dim / 2], or both NULL: no rotation */
+  const float* sin;
+  int n_positions;
+  const uint16_t* q_norm;  /* fp16 [head_dim], weights of a root-mean-square norm of each head, or NULL */
+  const uint16_t* k_norm;
+  float eps;
+  uint16_t* q_out;         /* fp16 [n_tokens][n_q_heads][head_dim], 4-byte aligned */
+} qtea_kv_append_args;
+
+/*
+ * Write a batch's new tokens into the cache, and prepare their queries, in one launch:
+ *   x = x * rsqrt(mean(x^2) + eps) * weight       (q and k, per head, where a weight is given)
+ *   (a, b) = (x[i], x[i + head_dim/2]):  (a cos - b sin, b cos + a sin)   (q and k, i < head_dim/2,
+ *                                        the table's row being the token's position)
+ * k and v are stored in the cache's format (fp16 saturates at +-65504; NaN stays NaN in fp16 and
+ * FP8 and becomes the largest code in FP4), q as fp16. All arithmetic is fp32, each product and sum of the rotation
+ * rounded by itself. Tokens whose position is negative, or whose page number is outside the cache,
+ * are not stored. Positions past the tables use their last row. Pages may be shared
+ * between sequences only where no two tokens of a call go to the same place.
+ * q, k, v, cos, sin: aligned to their element; strides at least the row's length. Returns QTEA_OK,
+ * QTEA_ERR_INVALID_ARG or QTEA_ERR_CUDA.
+ */
+int qtea_kv_append(const qtea_kv* kv, const qtea_kv_batch* batch, const qtea_kv_append_args* args,
+                   qtea_stream_t stream);
+
+/*
+ * Read sequences back as fp16: token p of sequence s goes to row row_start[s] + p of k_out and
+ * v_out ([n_rows][n_kv_heads][head_dim], 16-byte aligned; either may be NULL) for p < ctx_len[s]; the rest of
+ * the rows before row_start[s+1] are set to zero. row_start: device int32 [n_seqs + 1], ascending.
+ * Of the batch, q_start, n_tokens and max_q_len are not looked at. Rows in no sequence are not
+ * written. Tokens whose page number is outside the cache read as zero.
+ */
+int qtea_kv_read(const qtea_kv* kv, const qtea_kv_batch* batch, const int32_t* row_start, int n_rows, uint16_t* k_out,
+                 uint16_t* v_out, qtea_stream_t stream);
+
+/*
+ * Attention of a batch's new tokens over the cache (which already holds them):
+ *   out[t][h] = sum_j p_j v_j / sum_j p_j,   p_j = exp(scale * (q[t][h] . k_j) - m),
+ * over the tokens j of t's own sequence with j <= pos and, for window > 0, j > pos - window, where
+ * pos is t's position; m is any bound that keeps p in range. Query head h reads cache head
+ * h / (n_q_heads / n_kv_heads). A token that sees nothing (a negative position) gets zeros and
+ * lse = -infinity. Rows of the cache that a sequence does not hold never reach a result, whatever
+ * their bits.
+ *   q    device fp16, row t at t * q_ld: [n_q_heads][head_dim]; 4-byte aligned, q_ld even
+ *   out  device fp16, row t at t * out_ld, as q; 4-byte aligned, out_ld even; may be q itself
+ *   lse  device fp32 [n_tokens][n_q_heads], log of sum_j exp(scale * (q . k_j)), or NULL
+ *   n_q_heads   a multiple of n_kv_heads, at most 32 query heads for each
+ *   workspace   device memory of at least qtea_attention_workspace() bytes, 256-byte aligned, zeroed once
+ *               before its first use; each call leaves it ready for the next one, whatever its
+ *               sizes. Calls that share a workspace must be ordered on one stream.
+ * Products are fp16 x fp16 summed in fp32, the softmax's statistics are fp32, its weights are
+ * rounded to fp16 before the second product. Results are bitwise reproducible for given inputs and device.
+ * Returns QTEA_OK, QTEA_ERR_INVALID_ARG, QTEA_ERR_UNSUPPORTED (more than 32 query heads for one)
+ * or QTEA_ERR_CUDA.
+ */
+int qtea_attention(const qtea_kv* kv, const qtea_kv_batch* batch, const uint16_t* q, long long q_ld, int n_q_heads,
+                   float scale, int window, uint16_t* out, long long out_ld, float* lse, void* workspace,
+                   size_t workspace_bytes, qtea_stream_t stream);
+
+/* The workspace that qtea_attention needs on the current device for any batch over any cache. */
+int qtea_attention_workspace(size_t* bytes);
+
+/* QTEA_OK, or QTEA_ERR_TIMEOUT if a bounded wait in a kernel that used this workspace gave up (that
+ * call's output is then unspecified). Synchronizes `stream`; a workspace with a timeout is set back
+ * to zero. */
+int qtea_attention_status(void* workspace, size_t workspace_bytes, qtea_stream_t stream);
+
+/* Arguments of qtea_norm: rows of n_cols elements, row r of an array at r * ld. */
+typedef struct qtea_norm_args {
+  const void* h;               /* [n_rows][n_cols], the residual stream */
+  const void* y;               /* the block's output, or NULL: the norm before a block alone */
+  const uint16_t* post_weight; /* fp16 [n_cols], weight of the norm after the block, or NULL */
+  const uint16_t* gate;        /* fp16, row r at r * gate_ld (gate_ld = 0: one row for all), or NULL */
+  const uint16_t* weight;      /* fp16 [n_cols], weight of the norm before the next block */
+  void* h_out;                 /* as h (may be h itself), written when y is given */
+  uint16_t* x;                 /* fp16 [n_rows][n_cols], the next block's input, or NULL (then weight may be NULL) */
+  long long h_ld, y_ld, gate_ld, h_out_ld, x_ld;
+  int h_type, y_type;          /* QTEA_TYPE_* */
+  int n_rows, n_cols;
+  float res_scale, eps;
+} qtea_norm_args;
+
+/*
+ * The norms around a block with its gate and residual scale, in one launch. Per row:
+ *   t = y;  t = t * rsqrt(mean(t^2) + eps) * post_weight   (where given);  t = t * gate   (where given)
+ *   h' = h + res_scale * t      (h' = h without y)
+ *   x = h' * rsqrt(mean(h'^2) + eps) * weight
+ * in fp32; x from h' before it is rounded to h's type. The mean squares are sums of fp32 squares:
+ * magnitudes up to 2^56 or so are in range. Any n_rows >= 0, 1 <= n_cols <= 2^20, any alignment of
+ * the element (16-byte aligned arrays and strides with n_cols a multiple of 8 are the fast case).
+ * Returns QTEA_OK, QTEA_ERR_INVALID_ARG or QTEA_ERR_CUDA.
+ */
+int qtea_norm(const qtea_norm_args* args, qtea_stream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -13,6 +13,9 @@ import os
 from typing import Optional
 
 from . import build as _build
+from .decoder import (QTEA_KV_F16, QTEA_KV_FP4, QTEA_KV_FP8, QTEA_TYPE_F16, QTEA_TYPE_F32, KVBatch, KVCache,  # noqa: F401
+                      _bind as _bind_decoder, attention_workspace, qtea_attention, qtea_attention_status,
+                      qtea_kv_append, qtea_kv_read, qtea_norm)
 
 QTEA_OK = 0
 QTEA_ERR_INVALID_ARG = 1
@@ -103,6 +106,7 @@ def load(build_if_missing: bool = True):
     lib.qtea_quantize.argtypes = [P, P, i32, i32, i32, i32, i32, i32, i32, P, P, P, P, P, P, P]
     lib.qtea_probe_decode_rates.restype = i32
     lib.qtea_probe_decode_rates.argtypes = [P, i32]
+    _bind_decoder(lib)
     _lib = lib
     return lib
 

@@ -1,0 +1,682 @@
+// Attention of a few query rows per cache head over the paged cache (decode steps, drafted tokens),
+// and the entry points of qtea_attention.
+//
+// With R query rows sharing a cache head (tokens x query heads of the group, R <= 32) each cached
+// byte meets 2R multiply-adds at most: the kernel is bound by reading the cache, so its form
+// follows the copies. A warp works alone: it has its own ring of stages (8 KB of keys and values each at
+// head_dim 128), which its lanes refill with TMA boxes of 16 tokens, swizzled as the fragment loads
+// want them, and takes every fourth unit of the CTA's run. Nothing synchronises the CTA until its
+// four warps' results are joined at the end of an item.
+//
+// Products run transposed on mma.sync m16n8k16: S^T = K Q^T with keys as the 16 rows and query rows as
+// the 8 columns, O^T = V^T P^T with head_dim as the rows. A group of 4 to 8 query heads then fills a
+// whole column tile, where queries as rows would leave 8 to 12 of 16 empty; an accumulator of O takes half the
+// registers; and softmax weights pass from S^T's layout to P^T's with two movmatrix per 16 keys.
+// The order of head_dim inside a product is free as long as both sides agree, so codes are used in
+// the order in which ldmatrix leaves them in a thread: E4M3 and E2M1 become fp16 by one conversion
+// per pair and one exact multiplication by their block's power of two.
+//
+// The softmax runs in the base-2 domain against a reference that trails the running maximum by at
+// most kLag: weights are at most 2^kLag (fp16 holds them as precisely as those below 1), and the
+// accumulator is rescaled, and the row's maximum formed across lanes, only when the maximum
+// outruns the reference, a vote per 16 keys otherwise.
+#include <algorithm>
+#include <cstring>
+
+#include "qtea_attn.h"
+
+namespace qtea {
+namespace {
+
+constexpr int kWarps = 4;
+constexpr float kLag = 8.f;
+constexpr int kRowsGrid = 320;  // the weights of that many parts fit the rings
+constexpr float kNegInf = -INFINITY;
+
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+__device__ __forceinline__ void ldmatrix4(uint32_t* r, uint32_t addr) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+               : "r"(addr)
+               : "memory");
+}
+__device__ __forceinline__ void ldmatrix4_trans(uint32_t* r, uint32_t addr) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+               : "r"(addr)
+               : "memory");
+}
+__device__ __forceinline__ uint32_t transpose8(uint32_t a) {
+  uint32_t r;
+  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(a));
+  return r;
+}
+__device__ __forceinline__ void mma16816(float* c, const uint32_t* a, uint32_t b0, uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst),
+               "l"(reinterpret_cast<uint64_t>(src)), "r"(bytes), "r"(bar)
+               : "memory");
+}
+__device__ __forceinline__ uint32_t lds32(uint32_t a) {
+  uint32_t r;
+  asm volatile("ld.shared.u32 %0, [%1];" : "=r"(r) : "r"(a) : "memory");
+  return r;
+}
+__device__ __forceinline__ uint32_t lds16(uint32_t a) {
+  uint16_t r;
+  asm volatile("ld.shared.u16 %0, [%1];" : "=h"(r) : "r"(a) : "memory");
+  return r;
+}
+
+// Powers of two of block `blk` of two rows' scale words, as a pair of fp16 (see scale_bits).
+__device__ __forceinline__ uint32_t scale_pair(uint32_t w0, uint32_t w1, int blk) {
+  const uint32_t t = __byte_perm(w0, w1, blk | (4 + blk) << 8);  // in bytes 0 and 2, others beside them
+  return ((t & 0x001f001fu) ^ 0x00100010u) << 10;
+}
+
+template <int FMT, int D, int NT>
+struct Rows {
+  static constexpr int kKeys = FMT == QTEA_KV_F16 ? 16 : FMT == QTEA_KV_FP8 ? 32 : 64;  // of a unit
+  static constexpr int kShift = FMT == QTEA_KV_F16 ? 4 : FMT == QTEA_KV_FP8 ? 5 : 6;
+  static constexpr int kRowBytes = FMT == QTEA_KV_F16 ? 2 * D : FMT == QTEA_KV_FP8 ? D : D / 2;
+  static constexpr int kWide = kRowBytes < 128 ? kRowBytes : 128;  // bytes of a box's row
+  static constexpr int kParts = kRowBytes / kWide;
+  static constexpr int kBoxes = kKeys / 16;
+  static constexpr int kBoxBytes = 16 * kWide;
+  static constexpr int kSideBytes = kKeys * kRowBytes;
+  static constexpr int kScaleRow = D / kKvBlock;
+  static constexpr int kScaleBytes = FMT == QTEA_KV_F16 ? 0 : kKeys * kScaleRow;
+  static constexpr int kStageBytes = 2 * kSideBytes;
+  static constexpr int kStages = NT == 4 && D == 128 ? 2 : 3;  // two CTAs' rings fit an SM
+  static constexpr int kMaskXor = kWide == 128 ? 7 : kWide == 64 ? 3 : 1;
+  static constexpr int kRing = kWarps * kStages * kStageBytes;
+  static constexpr int kScaleRing = kWarps * kStages * 2 * kScaleBytes;
+};
+
+// Byte x of row r of a box, as the copy's swizzle placed it.
+template <class T>
+__device__ __forceinline__ uint32_t swizzled(int r, int x) {
+  const uint32_t off = r * T::kWide + x;
+  return off ^ (((off >> 7) & T::kMaskXor) << 4);
+}
+
+// NT column tiles of 8 query rows.
+template <int FMT, int D, int NT>
+__global__ void __launch_bounds__(kWarps * 32, 2)
+    qtea_attn_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
+                          const AttnParams p) {
+  using T = Rows<FMT, D, NT>;
+  constexpr int R = 8 * NT, KS = D / 16, MT = D / 16;
+  extern __shared__ __align__(1024) uint8_t smem[];  // the rings, then reused to join results
+  __shared__ long long prefix[kKvMaxSeqs + 1];
+  __shared__ __align__(8) uint64_t full[kWarps][T::kStages];
+  __shared__ float stat_m[kWarps][R], stat_l[kWarps][R], joined_m[R], joined_l[R];
+  __shared__ int is_last;
+  // Q^T fragments of four column tiles do not fit the registers beside O^T: they are read from here
+  constexpr bool kQShared = NT == 4;
+  __shared__ uint2 q_shared[kQShared ? KS * NT * 32 : 1];
+
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, c = lane & 3;
+  if (lane == 0) {
+#pragma unroll
+    for (int i = 0; i < T::kStages; ++i) mbar_init(smem_u32(&full[warp][i]), 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  attn_prefix(p, prefix);
+  const AttnSplit split = attn_split(p, prefix);
+  if (split.total == 0 || (int)blockIdx.x >= split.ctas) return;
+  const long long end = split.first(blockIdx.x + 1);
+
+  const uint32_t ring = smem_u32(smem) + warp * T::kStages * T::kStageBytes;
+  const uint32_t scales = smem_u32(smem) + T::kRing + warp * T::kStages * 2 * T::kScaleBytes;
+  float* join = reinterpret_cast<float*>(smem);
+  uint32_t fills = 0;  // stages this warp has consumed, over all items
+  bool ok = true;
+
+  for (long long cur = split.first(blockIdx.x); cur < end;) {
+    const AttnItem it = attn_item(p, prefix, cur, end);
+    cur += it.units;
+    const int mine = (it.units - warp + kWarps - 1) / kWarps;  // units unit0 + warp + kWarps * i
+    const int* pages = p.b.pages + (long long)it.s * p.b.max_pages;
+
+    // The copies of this warp's unit i: a box of 16 tokens per lane. Its page number was loaded
+    // when the box before it was issued.
+    auto page_of = [&](int i) {
+      const int key = ((it.unit0 + warp + kWarps * i) << T::kShift) + 16 * lane;
+      return __ldg(pages + min(key >> p.kv.page_shift, p.b.max_pages - 1));
+    };
+    int next_page = lane < T::kBoxes && mine > 0 ? page_of(0) : 0;
+    auto issue = [&](int i, uint32_t stage) {
+      const uint32_t bar = smem_u32(&full[warp][stage]);
+      if (lane == 0) mbar_arrive_expect_tx(bar, T::kStageBytes + 2 * T::kScaleBytes);
+      __syncwarp();
+      if (lane < T::kBoxes) {
+        const int key = ((it.unit0 + warp + kWarps * i) << T::kShift) + 16 * lane;
+        const int page = min(max(next_page, 0), p.kv.n_pages - 1);
+        const int row = (page * p.kv.heads + it.head) * p.kv.page_size + (key & (p.kv.page_size - 1));
+        const uint32_t dst = ring + stage * T::kStageBytes + lane * T::kParts * T::kBoxBytes;
+#pragma unroll
+        for (int h = 0; h < T::kParts; ++h) tma_load_2d(dst + h * T::kBoxBytes, &map_k, h * T::kWide, row, bar);
+#pragma unroll
+        for (int h = 0; h < T::kParts; ++h)
+          tma_load_2d(dst + T::kSideBytes + h * T::kBoxBytes, &map_v, h * T::kWide, row, bar);
+        if (FMT != QTEA_KV_F16) {
+          const uint32_t sd = scales + stage * 2 * T::kScaleBytes + lane * 16 * T::kScaleRow;
+          bulk_load(sd, p.kv.ks + (long long)row * T::kScaleRow, 16 * T::kScaleRow, bar);
+          bulk_load(sd + T::kScaleBytes, p.kv.vs + (long long)row * T::kScaleRow, 16 * T::kScaleRow, bar);
+        }
+        if (i + 1 < mine) next_page = page_of(i + 1);
+      }
+    };
+    uint32_t st_issue = fills % T::kStages;
+    for (int i = 0; i < min(mine, T::kStages); ++i) {
+      issue(i, st_issue);
+      st_issue = st_issue + 1 == T::kStages ? 0 : st_issue + 1;
+    }
+
+    // This thread's query rows: 8 nt + 2c and the next (columns of S^T and O^T), and the keys that
+    // each sees, [lo, hi).
+    const int i0 = it.tile * p.tile_tokens, rows = min(it.seq.n - i0, p.tile_tokens) * p.group;
+    int lo[NT][2], hi[NT][2];
+    int lo_all = 0x7fffffff, hi_all = 0, lo_in = 0, hi_in = 0x7fffffff;
+    for (int r = 0; r < rows; r += p.group) {  // once per token: uniform bounds over the tile
+      const int pos = it.seq.base + i0 + r / p.group;
+      const int l = p.window > 0 ? max(0, pos - p.window + 1) : 0, h = pos + 1;
+      lo_all = min(lo_all, l), hi_all = max(hi_all, h), lo_in = max(lo_in, l), hi_in = min(hi_in, h);
+    }
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int r = 8 * nt + 2 * c + e, pos = it.seq.base + i0 + r / p.group;
+        hi[nt][e] = r < rows ? pos + 1 : 0;
+        lo[nt][e] = p.window > 0 ? max(0, pos - p.window + 1) : 0;
+      }
+
+    // Q^T fragments: column (query row) 8 nt + g, head_dim in the order of the format's codes.
+    uint2 qf[kQShared ? 1 : KS][NT];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      const int r = 8 * nt + g, tok = it.seq.q0 + i0 + r / p.group, h = it.head * p.group + r % p.group;
+      const __half* row = p.q + (long long)tok * p.q_ld + (long long)h * D;
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        if (kQShared && ks % kWarps != warp) continue;  // the warps share the loads
+        const int d0 = FMT == QTEA_KV_F16   ? 16 * ks + 2 * c
+                       : FMT == QTEA_KV_FP8 ? 16 * ks + 4 * c
+                                            : 32 * (ks >> 1) + 8 * c + 4 * (ks & 1);
+        const int d1 = d0 + (FMT == QTEA_KV_F16 ? 8 : 2);
+        uint2 v = make_uint2(0u, 0u);
+        if (r < rows) {
+          v.x = *reinterpret_cast<const uint32_t*>(row + d0);
+          v.y = *reinterpret_cast<const uint32_t*>(row + d1);
+        }
+        if (kQShared) q_shared[(ks * NT + nt) * 32 + lane] = v;
+        else qf[kQShared ? 0 : ks][nt] = v;
+      }
+    }
+    if (kQShared) __syncthreads();
+    auto mma_q = [&](float* acc, const uint32_t* a, int ks, int nt) {
+      const uint2 b = kQShared ? q_shared[(ks * NT + nt) * 32 + lane] : qf[kQShared ? 0 : ks][nt];
+      mma16816(acc, a, b.x, b.y);
+    };
+
+    float o[MT][NT][4];
+    float m[NT][2], l[NT][2];  // the reference (-infinity while nothing has been seen) and this thread's sums
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) m[nt][0] = m[nt][1] = kNegInf, l[nt][0] = l[nt][1] = 0.f;
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[mt][nt][e] = 0.f;
+
+    for (int i = 0; i < mine && ok; ++i) {
+      const uint32_t stage = fills % T::kStages;
+      ok = mbar_wait(smem_u32(&full[warp][stage]), (fills / T::kStages) & 1, p.status);
+      if (!ok) break;
+      const uint32_t kbase = ring + stage * T::kStageBytes, vbase = kbase + T::kSideBytes;
+      const uint32_t sbase = scales + stage * 2 * T::kScaleBytes;
+      const int key_unit = (it.unit0 + warp + kWarps * i) << T::kShift;
+#pragma unroll 1
+      for (int sub = 0; sub < T::kBoxes; ++sub) {
+        const int key0 = key_unit + 16 * sub;
+        if (key0 >= hi_all || key0 + 16 <= lo_all) continue;  // nothing of the tile sees these
+        const uint32_t kb = kbase + sub * T::kParts * T::kBoxBytes, vb = vbase + sub * T::kParts * T::kBoxBytes;
+        float s[NT][4];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) s[nt][0] = s[nt][1] = s[nt][2] = s[nt][3] = 0.f;
+        {
+          const int kr = (lane & 7) + (lane >> 3 & 1) * 8, kx = (lane >> 4) * 16;
+          if (FMT == QTEA_KV_F16) {
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) {
+              const int x = 32 * ks;
+              uint32_t a[4];
+              ldmatrix4(a, kb + (x / T::kWide) * T::kBoxBytes + swizzled<T>(kr, x % T::kWide + kx));
+#pragma unroll
+              for (int nt = 0; nt < NT; ++nt) mma_q(s[nt], a, ks, nt);
+            }
+          } else {
+            const uint32_t sk = sbase + sub * 16 * T::kScaleRow;
+            const uint32_t w0 = D == 128 ? lds32(sk + g * 4) : lds16(sk + g * 2);
+            const uint32_t w1 = D == 128 ? lds32(sk + (g + 8) * 4) : lds16(sk + (g + 8) * 2);
+#pragma unroll
+            for (int x = 0; x < T::kRowBytes; x += 32) {
+              uint32_t r[4];
+              ldmatrix4(r, kb + swizzled<T>(kr, x + kx));
+              if (FMT == QTEA_KV_FP8) {
+                const int blk = x / 32;
+                const uint32_t f0 = scale_pair(w0, w0, blk), f1 = scale_pair(w1, w1, blk);
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                  const uint32_t a[4] = {hmul2(from_e4m3x2(r[2 * j]), f0), hmul2(from_e4m3x2(r[2 * j + 1]), f1),
+                                         hmul2(from_e4m3x2_hi(r[2 * j]), f0), hmul2(from_e4m3x2_hi(r[2 * j + 1]), f1)};
+#pragma unroll
+                  for (int nt = 0; nt < NT; ++nt) mma_q(s[nt], a, 2 * blk + j, nt);
+                }
+              } else {
+#pragma unroll
+                for (int hb = 0; hb < 2; ++hb) {
+                  const int blk = x / 16 + hb;
+                  if (blk >= D / 32) break;
+                  const uint32_t f0 = scale_pair(w0, w0, blk), f1 = scale_pair(w1, w1, blk);
+                  uint32_t e0[4], e1[4];
+                  from_e2m1x8(r[2 * hb], e0);
+                  from_e2m1x8(r[2 * hb + 1], e1);
+#pragma unroll
+                  for (int j = 0; j < 2; ++j) {
+                    const uint32_t a[4] = {hmul2(e0[2 * j], f0), hmul2(e1[2 * j], f1), hmul2(e0[2 * j + 1], f0),
+                                           hmul2(e1[2 * j + 1], f1)};
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) mma_q(s[nt], a, 2 * blk + j, nt);
+                  }
+                }
+              }
+            }
+          }
+        }
+        // softmax weights
+        const bool masked = key0 + 16 > hi_in || key0 < lo_in;
+        bool outrun = false;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            s[nt][e] *= p.scale_log2;
+            if (masked) {
+              const int key = key0 + g + (e >> 1) * 8;
+              if (key < lo[nt][e & 1] || key >= hi[nt][e & 1]) s[nt][e] = kNegInf;
+            }
+            outrun |= s[nt][e] > m[nt][e & 1] + kLag;
+          }
+        if (__any_sync(0xffffffffu, outrun)) {
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              float top = fmaxf(s[nt][e], s[nt][e + 2]);
+              top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 4));
+              top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 8));
+              top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16));
+              const float next = fmaxf(m[nt][e], top);
+              const float f = next == kNegInf ? 1.f : ex2(m[nt][e] - next);
+              m[nt][e] = next;
+              l[nt][e] *= f;
+#pragma unroll
+              for (int mt = 0; mt < MT; ++mt) o[mt][nt][e] *= f, o[mt][nt][e + 2] *= f;
+            }
+        }
+        uint32_t pf[NT][2];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const float ref = m[nt][e] == kNegInf ? 0.f : m[nt][e];
+            s[nt][e] = ex2(s[nt][e] - ref);
+            s[nt][e + 2] = ex2(s[nt][e + 2] - ref);
+            l[nt][e] += s[nt][e] + s[nt][e + 2];
+          }
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const __half2 w = __floats2half2_rn(s[nt][2 * h], s[nt][2 * h + 1]);
+            pf[nt][h] = transpose8(*reinterpret_cast<const uint32_t*>(&w));
+          }
+        }
+        // O^T += V^T P^T. Where some keys lie outside all that the tile sees, their values are
+        // replaced by zeros: 0 * NaN would reach the sums.
+        uint32_t keep0 = 0xffffffffu, keep1 = 0xffffffffu;  // of keys 2c, 2c+1 and 2c+8, 2c+9
+        if (key0 + 16 > hi_all || key0 < lo_all) {
+          auto in = [&](int k) { return key0 + k >= lo_all && key0 + k < hi_all; };
+          keep0 = (in(2 * c) ? 0xffffu : 0u) | (in(2 * c + 1) ? 0xffff0000u : 0u);
+          keep1 = (in(2 * c + 8) ? 0xffffu : 0u) | (in(2 * c + 9) ? 0xffff0000u : 0u);
+        }
+        {
+          const int vr = (lane & 7) + (lane >> 4) * 8, vx = (lane >> 3 & 1) * 16;
+          if (FMT == QTEA_KV_F16) {
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) {
+              const int x = 32 * mt;
+              uint32_t a[4];
+              ldmatrix4_trans(a, vb + (x / T::kWide) * T::kBoxBytes + swizzled<T>(vr, x % T::kWide + vx));
+              a[0] &= keep0, a[1] &= keep0, a[2] &= keep1, a[3] &= keep1;
+#pragma unroll
+              for (int nt = 0; nt < NT; ++nt) mma16816(o[mt][nt], a, pf[nt][0], pf[nt][1]);
+            }
+          } else {
+            const uint32_t sv = sbase + T::kScaleBytes + sub * 16 * T::kScaleRow;
+            uint32_t w[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const int key = 2 * c + (j & 1) + (j >> 1) * 8;
+              w[j] = D == 128 ? lds32(sv + key * 4) : lds16(sv + key * 2);
+            }
+#pragma unroll
+            for (int x = 0; x < T::kRowBytes; x += 32) {
+              uint32_t r[4];
+              ldmatrix4_trans(r, vb + swizzled<T>(vr, x + vx));
+              if (FMT == QTEA_KV_FP8) {
+                const int blk = x / 32;
+                const uint32_t f0 = scale_pair(w[0], w[1], blk), f1 = scale_pair(w[2], w[3], blk);
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {  // codes 16 j + 2g and the next
+                  const uint32_t t0 = __byte_perm(r[j], 0, 0x3120), t1 = __byte_perm(r[2 + j], 0, 0x3120);
+                  const uint32_t a[4] = {hmul2(from_e4m3x2(t0), f0) & keep0, hmul2(from_e4m3x2_hi(t0), f0) & keep0,
+                                         hmul2(from_e4m3x2(t1), f1) & keep1, hmul2(from_e4m3x2_hi(t1), f1) & keep1};
+#pragma unroll
+                  for (int nt = 0; nt < NT; ++nt) mma16816(o[2 * blk + j][nt], a, pf[nt][0], pf[nt][1]);
+                }
+              } else {
+#pragma unroll
+                for (int hb = 0; hb < 2; ++hb) {
+                  const int blk = x / 16 + hb;
+                  if (blk >= D / 32) break;
+                  const uint32_t f0 = scale_pair(w[0], w[1], blk), f1 = scale_pair(w[2], w[3], blk);
+                  uint32_t e0[4], e1[4];
+                  from_e2m1x8(r[hb], e0);
+                  from_e2m1x8(r[2 + hb], e1);
+#pragma unroll
+                  for (int j = 0; j < 2; ++j) {  // codes 4g + 2j and the next
+                    const uint32_t a[4] = {hmul2(__byte_perm(e0[j], e0[2 + j], 0x5410), f0) & keep0,
+                                           hmul2(__byte_perm(e0[j], e0[2 + j], 0x7632), f0) & keep0,
+                                           hmul2(__byte_perm(e1[j], e1[2 + j], 0x5410), f1) & keep1,
+                                           hmul2(__byte_perm(e1[j], e1[2 + j], 0x7632), f1) & keep1};
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) mma16816(o[2 * blk + j][nt], a, pf[nt][0], pf[nt][1]);
+                  }
+                }
+              }
+            }
+          }
+        }
+      }
+      ++fills;
+      __syncwarp();  // every lane is done with the stage
+      if (i + T::kStages < mine) issue(i + T::kStages, stage);
+    }
+
+    // Join the warps' results: each leaves O^T [D][R], m and l in the rings' memory.
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        float v = l[nt][e];
+        v += __shfl_xor_sync(0xffffffffu, v, 4);
+        v += __shfl_xor_sync(0xffffffffu, v, 8);
+        v += __shfl_xor_sync(0xffffffffu, v, 16);
+        l[nt][e] = v;
+      }
+    ok = __syncthreads_and(ok);  // all copies have landed and been read
+    if (!ok) return;             // a copy never came: the status word says so
+    {
+      float* w = join + warp * D * R;
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt) {
+        const int d0 = FMT == QTEA_KV_F16   ? 16 * mt + g
+                       : FMT == QTEA_KV_FP8 ? 16 * mt + 2 * g
+                                            : 32 * (mt >> 1) + 4 * g + 2 * (mt & 1);
+        const int d1 = d0 + (FMT == QTEA_KV_F16 ? 8 : 1);
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          *reinterpret_cast<float2*>(w + d0 * R + 8 * nt + 2 * c) = make_float2(o[mt][nt][0], o[mt][nt][1]);
+          *reinterpret_cast<float2*>(w + d1 * R + 8 * nt + 2 * c) = make_float2(o[mt][nt][2], o[mt][nt][3]);
+        }
+      }
+      if (g == 0) {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            stat_m[warp][8 * nt + 2 * c + e] = m[nt][e];
+            stat_l[warp][8 * nt + 2 * c + e] = l[nt][e];
+          }
+      }
+    }
+    __syncthreads();
+    if (threadIdx.x < R) {  // each warp's weight, in the place of its m
+      const int r = threadIdx.x;
+      float top = kNegInf, sum = 0.f;
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) top = fmaxf(top, stat_m[w][r]);
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) {
+        const float f = top == kNegInf ? 0.f : ex2(stat_m[w][r] - top);
+        stat_m[w][r] = f;
+        sum = fmaf(stat_l[w][r], f, sum);
+      }
+      joined_m[r] = top;
+      joined_l[r] = sum;
+    }
+    __syncthreads();
+
+    const int c0 = split.cta_of(it.item_first), c1 = split.cta_of(it.item_first + it.item_units - 1);
+    auto write_out = [&](int r, int d, float v) {
+      const int tok = it.seq.q0 + i0 + r / p.group, h = it.head * p.group + r % p.group;
+      p.out[(long long)tok * p.out_ld + (long long)h * D + d] = __float2half_rn(v);
+    };
+    auto write_lse = [&](int r, float top, float sum) {
+      const int tok = it.seq.q0 + i0 + r / p.group, h = it.head * p.group + r % p.group;
+      if (p.lse) p.lse[(long long)tok * p.q_heads + h] = sum > 0.f ? (top + log2f(sum)) * 0.6931471805599453f : sum == 0.f ? kNegInf : sum;
+    };
+    const size_t slot_floats = (size_t)D * R + 2 * R;
+    float* slot = p.slots + (2 * (size_t)blockIdx.x + ((int)blockIdx.x == c0 ? 1 : 0)) * slot_floats;
+    for (int e = threadIdx.x; e < D * R; e += kWarps * 32) {
+      const int r = e % R, d = e / R;
+      float v = 0.f;
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) v = fmaf(join[w * D * R + e], stat_m[w][r], v);
+      if (c0 == c1) {
+        if (r < rows) write_out(r, d, joined_l[r] == 0.f ? 0.f : v / joined_l[r]);
+      } else {
+        __stcg(slot + e, v);
+      }
+    }
+    if (c0 == c1) {
+      if (threadIdx.x < rows) write_lse(threadIdx.x, joined_m[threadIdx.x], joined_l[threadIdx.x]);
+    } else {
+      if (threadIdx.x < R) {
+        __stcg(slot + D * R + threadIdx.x, joined_m[threadIdx.x]);
+        __stcg(slot + D * R + R + threadIdx.x, joined_l[threadIdx.x]);
+      }
+      __threadfence();
+      __syncthreads();
+      if (threadIdx.x == 0) {
+        const unsigned before = atomicAdd(p.counters + c0, 1u);
+        is_last = before == (unsigned)(c1 - c0);
+        if (is_last) p.counters[c0] = 0;  // ready for the next call
+      }
+      __syncthreads();
+      if (is_last) {
+        __threadfence();
+        // the parts' weights, [part][row], then their sum in the parts' order
+        const int parts = c1 - c0 + 1;
+        auto part = [&](int i) {
+          return p.slots + (2 * (size_t)(c0 + i) + (i == 0 ? 1 : 0)) * slot_floats;
+        };
+        for (int e = threadIdx.x; e < parts * R; e += kWarps * 32) join[e] = __ldcg(part(e / R) + D * R + e % R);
+        __syncthreads();
+        if (threadIdx.x < R) {
+          const int r = threadIdx.x;
+          float top = kNegInf, sum = 0.f;
+          for (int i = 0; i < parts; ++i) top = fmaxf(top, join[i * R + r]);
+          for (int i = 0; i < parts; ++i) {
+            const float f = top == kNegInf ? 0.f : ex2(join[i * R + r] - top);
+            join[i * R + r] = f;
+            sum = fmaf(__ldcg(part(i) + D * R + R + r), f, sum);
+          }
+          joined_l[r] = sum;
+          if (r < rows) write_lse(r, top, sum);
+        }
+        __syncthreads();
+        for (int e = threadIdx.x; e < D * R; e += kWarps * 32) {
+          const int r = e % R, d = e / R;
+          if (r >= rows) continue;
+          float v = 0.f;
+#pragma unroll 8
+          for (int i = 0; i < parts; ++i) v = fmaf(__ldcg(part(i) + e), join[i * R + r], v);
+          write_out(r, d, joined_l[r] == 0.f ? 0.f : v / joined_l[r]);
+        }
+      }
+    }
+    // the next item's copies write where these reads and writes were
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    __syncthreads();
+  }
+}
+
+template <int FMT, int D, int NT>
+cudaError_t launch(const qtea_kv* kv, const AttnParams& p, int grid, cudaStream_t st) {
+  using T = Rows<FMT, D, NT>;
+  const int smem = T::kRing + T::kScaleRing;
+  static_assert(kWarps * D * 8 * NT * 4 <= T::kRing && kRowsGrid * 8 * NT * 4 <= T::kRing,
+                "what is joined fits the rings");
+  auto k = qtea_attn_rows_kernel<FMT, D, NT>;
+  cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  if (e != cudaSuccess) return e;
+  k<<<grid, kWarps * 32, smem, st>>>(kv->map_k, kv->map_v, p);
+  return cudaGetLastError();
+}
+
+template <int FMT, int D>
+cudaError_t launch_nt(const qtea_kv* kv, const AttnParams& p, int nt, int grid, cudaStream_t st) {
+  if (nt == 1) return launch<FMT, D, 1>(kv, p, grid, st);
+  if (nt == 2) return launch<FMT, D, 2>(kv, p, grid, st);
+  return launch<FMT, D, 4>(kv, p, grid, st);
+}
+
+template <int FMT>
+cudaError_t launch_dim(const qtea_kv* kv, const AttnParams& p, int nt, int grid, cudaStream_t st) {
+  return kv->view.dim == 128 ? launch_nt<FMT, 128>(kv, p, nt, grid, st) : launch_nt<FMT, 64>(kv, p, nt, grid, st);
+}
+
+constexpr int kMaxRows = 32;
+
+}  // namespace
+
+int attn_rows_grid(int sm_count) { return std::min(2 * sm_count, kRowsGrid); }
+
+size_t attn_rows_floats(int sm_count) { return (size_t)attn_rows_grid(sm_count) * (128 * kMaxRows + 2 * kMaxRows); }
+
+cudaError_t launch_attn_rows(const qtea_kv* kv, const AttnParams& base, cudaStream_t st) {
+  AttnParams p = base;
+  const int grid = attn_rows_grid(kv->sm_count);
+  // column tiles of 8 rows: the fewest that hold the longest sequence's rows, or whole tokens at 32
+  const long long rows = (long long)p.group * p.b.max_q;
+  const int nt = rows <= 8 ? 1 : rows <= 16 ? 2 : 4;
+  p.tile_tokens = 8 * nt / p.group;
+  p.unit_shift = kv->view.format == QTEA_KV_F16 ? 4 : kv->view.format == QTEA_KV_FP8 ? 5 : 6;
+  p.min_units = 2 * kWarps;
+  if (kv->view.format == QTEA_KV_F16) return launch_dim<QTEA_KV_F16>(kv, p, nt, grid, st);
+  if (kv->view.format == QTEA_KV_FP8) return launch_dim<QTEA_KV_FP8>(kv, p, nt, grid, st);
+  return launch_dim<QTEA_KV_FP4>(kv, p, nt, grid, st);
+}
+
+}  // namespace qtea
+
+using namespace qtea;
+
+namespace {
+bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
+
+size_t workspace_bytes_for(int sm_count) {
+  return kAttnHeaderBytes + 2 * sizeof(float) * attn_rows_floats(sm_count);
+}
+}  // namespace
+
+extern "C" {
+
+int qtea_attention_workspace(size_t* bytes) {
+  if (!bytes) return QTEA_ERR_INVALID_ARG;
+  int dev = 0, sms = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess ||
+      cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) {
+    cudaGetLastError();
+    return QTEA_ERR_CUDA;
+  }
+  *bytes = workspace_bytes_for(sms);
+  return QTEA_OK;
+}
+
+int qtea_attention(const qtea_kv* kv, const qtea_kv_batch* batch, const uint16_t* q, long long q_ld, int n_q_heads,
+                   float scale, int window, uint16_t* out, long long out_ld, float* lse, void* workspace,
+                   size_t workspace_bytes, qtea_stream_t stream) {
+  AttnParams p;
+  std::memset(&p, 0, sizeof(p));
+  int rc = check_batch(kv, batch, true, &p.b);
+  if (rc) return rc;
+  const KvView& c = kv->view;
+  if (n_q_heads < 1 || n_q_heads % c.heads != 0 || window < 0) return QTEA_ERR_INVALID_ARG;
+  p.group = n_q_heads / c.heads;
+  if (p.group > kAttnMaxGroup) return QTEA_ERR_UNSUPPORTED;
+  const long long row = (long long)n_q_heads * c.dim;
+  if (p.b.n_seqs == 0 || p.b.n_tokens == 0) return QTEA_OK;
+  if (!q || !out || q_ld < row || out_ld < row || q_ld % 2 || out_ld % 2 || !aligned(q, 4) || !aligned(out, 4) ||
+      !aligned(lse, 4))
+    return QTEA_ERR_INVALID_ARG;
+  if (!workspace || !aligned(workspace, 256) || workspace_bytes < workspace_bytes_for(kv->sm_count))
+    return QTEA_ERR_INVALID_ARG;
+  p.kv = c;
+  p.q = reinterpret_cast<const __half*>(q);
+  p.out = reinterpret_cast<__half*>(out);
+  p.lse = lse;
+  p.q_ld = q_ld, p.out_ld = out_ld;
+  p.q_heads = n_q_heads;
+  p.scale_log2 = scale * 1.4426950408889634f;
+  p.window = window;
+  p.status = static_cast<int*>(workspace);
+  p.counters = reinterpret_cast<unsigned*>(workspace) + 64;
+  p.slots = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + kAttnHeaderBytes);
+  cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+  if (launch_attn_rows(kv, p, st) != cudaSuccess) {
+    cudaGetLastError();
+    return QTEA_ERR_CUDA;
+  }
+  return QTEA_OK;
+}
+
+int qtea_attention_status(void* workspace, size_t workspace_bytes, qtea_stream_t stream) {
+  if (!workspace || workspace_bytes < (size_t)kAttnHeaderBytes) return QTEA_ERR_INVALID_ARG;
+  cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+  int flag = 0;
+  if (cudaMemcpyAsync(&flag, workspace, sizeof(int), cudaMemcpyDeviceToHost, st) != cudaSuccess ||
+      cudaStreamSynchronize(st) != cudaSuccess ||
+      (flag != 0 && (cudaMemsetAsync(workspace, 0, kAttnHeaderBytes, st) != cudaSuccess ||
+                     cudaStreamSynchronize(st) != cudaSuccess))) {
+    cudaGetLastError();
+    return QTEA_ERR_CUDA;
+  }
+  return flag == 0 ? QTEA_OK : flag;
+}
+
+}  // extern "C"

@@ -1,0 +1,127 @@
+// The paged key/value cache as its kernels see it, and the conversions of its formats.
+#pragma once
+
+#include <cuda_fp16.h>
+
+#include "qtea_internal.h"
+
+namespace qtea {
+
+constexpr int kKvBlock = 32;      // elements that share a power of two
+constexpr int kKvMaxSeqs = 1024;  // sequences of one call
+constexpr int kKvEMin = -14;      // every value is then a multiple of 2^-23: exact in fp16
+constexpr int kKvEMaxFp8 = 7;     // 448 * 2^7 = 57344
+constexpr int kKvEMaxFp4 = 13;    // 6 * 2^13 = 49152
+
+// The cache's arrays and sizes, by value into kernels.
+struct KvView {
+  uint8_t* k;
+  uint8_t* v;
+  uint8_t* ks;
+  uint8_t* vs;
+  int n_pages, page_size, heads, dim, format;
+  int page_shift;  // log2(page_size)
+};
+
+// The batch's arrays and sizes.
+struct KvBatchView {
+  const int32_t* q_start;
+  const int32_t* ctx_len;
+  const int32_t* pages;
+  int n_seqs, max_pages, n_tokens, max_q;
+};
+
+// Bytes of one cached row's codes.
+__host__ __device__ __forceinline__ int kv_row_bytes(int format, int dim) {
+  return format == QTEA_KV_F16 ? 2 * dim : format == QTEA_KV_FP8 ? dim : dim / 2;
+}
+
+int check_batch(const qtea_kv* kv, const qtea_kv_batch* b, bool queries, KvBatchView* out);
+
+#ifdef __CUDACC__
+// A sequence's context length as the kernels take it: within what its page table can name.
+__device__ __forceinline__ int kv_context(const KvBatchView& b, const KvView& kv, int s) {
+  const int most = b.max_pages << kv.page_shift;  // < 2^31 (checked on the host)
+  return min(max(__ldg(b.ctx_len + s), 0), most);
+}
+
+// The sequence whose rows [start[s], start[s+1]) hold `row`, found by one warp (all 32 lanes call
+// it, with the same row), or -1.
+__device__ __forceinline__ int kv_find_sequence(const int32_t* start, int n_seqs, int row) {
+  const int lane = threadIdx.x & 31;
+  if (row < __ldg(start)) return -1;
+  for (int base = 0; base < n_seqs; base += 32) {
+    const int s = base + lane;
+    const bool past = s < n_seqs && __ldg(start + s + 1) > row;
+    const unsigned m = __ballot_sync(0xffffffffu, past);
+    if (m) return base + __ffs(m) - 1;
+  }
+  return -1;
+}
+
+// The exponent of a block's power of two: the smallest e >= kKvEMin with top <= limit * 2^e, at most
+// e_max. limit = 1.75 * 2^8 (FP8) or 1.5 * 2^2 (FP4), so the comparison is one of mantissas.
+template <int FMT>
+__device__ __forceinline__ int kv_exponent(float top) {
+  constexpr uint32_t kMant = FMT == QTEA_KV_FP8 ? 0x600000u : 0x400000u;
+  constexpr int kShift = FMT == QTEA_KV_FP8 ? 8 : 2;
+  constexpr int kMax = FMT == QTEA_KV_FP8 ? kKvEMaxFp8 : kKvEMaxFp4;
+  const uint32_t u = __float_as_uint(top);  // top >= 0; infinity has the largest exponent
+  const int e = (int)(u >> 23) - 127 - kShift + ((u & 0x7fffffu) > kMant ? 1 : 0);
+  return min(max(e, kKvEMin), kMax);
+}
+
+// 2^e as fp32, -126 <= e <= 127.
+__device__ __forceinline__ float exp2i(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }
+
+// Two fp32 values to two codes: E4M3 bytes (a in the low one) or E2M1 nibbles (a in the low one).
+__device__ __forceinline__ uint32_t to_e4m3x2(float a, float b) {
+  uint16_t r;
+  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(b), "f"(a));
+  return r;
+}
+__device__ __forceinline__ uint32_t to_e2m1x2(float a, float b) {
+  uint32_t r;
+  asm("{ .reg .b8 t; cvt.rn.satfinite.e2m1x2.f32 t, %1, %2; cvt.u32.u8 %0, t; }" : "=r"(r) : "f"(b), "f"(a));
+  return r;
+}
+
+// Two codes to two fp16 values (exact).
+__device__ __forceinline__ uint32_t from_e4m3x2(uint32_t lo16) {
+  uint32_t r;
+  asm("{ .reg .b16 t, u; mov.b32 {t, u}, %1; cvt.rn.f16x2.e4m3x2 %0, t; }" : "=r"(r) : "r"(lo16));
+  return r;
+}
+__device__ __forceinline__ uint32_t from_e4m3x2_hi(uint32_t hi16) {
+  uint32_t r;
+  asm("{ .reg .b16 t, u; mov.b32 {t, u}, %1; cvt.rn.f16x2.e4m3x2 %0, u; }" : "=r"(r) : "r"(hi16));
+  return r;
+}
+// All four bytes of a word of E2M1 codes: out[i] = byte i's two values.
+__device__ __forceinline__ void from_e2m1x8(uint32_t w, uint32_t* out) {
+  asm("{ .reg .b8 a, b, c, d; mov.b32 {a, b, c, d}, %4;\n"
+      "  cvt.rn.f16x2.e2m1x2 %0, a; cvt.rn.f16x2.e2m1x2 %1, b;\n"
+      "  cvt.rn.f16x2.e2m1x2 %2, c; cvt.rn.f16x2.e2m1x2 %3, d; }"
+      : "=r"(out[0]), "=r"(out[1]), "=r"(out[2]), "=r"(out[3])
+      : "r"(w));
+}
+
+__device__ __forceinline__ uint32_t hmul2(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+
+// fp16 bits of the power of two that a scale byte stands for (113..142 in a cache that append
+// wrote; other bytes, in rows that nothing wrote, give some fp16 value).
+__device__ __forceinline__ uint32_t scale_bits(uint32_t byte) { return ((byte - 112u) & 31u) << 10; }
+#endif
+
+}  // namespace qtea
+
+struct qtea_kv {
+  qtea::KvView view;
+  int device, sm_count;
+  // Tensor maps of the codes, rows of 64 or 128 bytes ... (see qtea_attn.cu, qtea_attn_chunk.cu)
+  CUtensorMap map_k, map_v;
+};

@@ -1,0 +1,326 @@
+// The norms before and after a block, fused with the block's gate and residual scale (qtea_norm).
+//
+// Per row of n columns: t = y [* rsqrt(mean t^2 + eps) * post] [* gate], h' = h + r t,
+// x = h' * rsqrt(mean h'^2 + eps) * w. Two sums over the row that depend on one another, and every
+// element is needed again after each: a CTA takes a row, reads each element once, keeps it in
+// registers (8 elements per thread and chunk) and joins its sums through shared memory, one barrier
+// per sum. Bound by memory at many rows, by the latency of one load, two sums and a store at few.
+#include <cuda_fp16.h>
+
+#include <algorithm>
+
+#include "qtea_internal.h"
+
+namespace qtea {
+namespace {
+
+struct NormParams {
+  const void* h;
+  const void* y;
+  const __half* post;
+  const __half* gate;
+  const __half* weight;
+  void* h_out;
+  __half* x;
+  long long h_ld, y_ld, gate_ld, h_out_ld, x_ld;
+  int n_rows, n;
+  float res_scale, eps;
+};
+
+constexpr int kNone = -1;
+template <int C>
+constexpr int kNormThreads = C == 1 ? 1024 : 512;  // most threads of a CTA: the registers hold the row
+
+template <int TYPE>
+__device__ __forceinline__ float load1(const void* p, size_t i) {
+  if (TYPE == QTEA_TYPE_F32) return static_cast<const float*>(p)[i];
+  return __half2float(static_cast<const __half*>(p)[i]);
+}
+
+__device__ __forceinline__ void unpack8(const uint4& u, float* v) {
+  const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
+    v[2 * i] = f.x;
+    v[2 * i + 1] = f.y;
+  }
+}
+
+__device__ __forceinline__ uint4 pack8(const float* v) {
+  uint32_t w[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const __half2 h = __floats2half2_rn(v[2 * i], v[2 * i + 1]);
+    w[i] = *reinterpret_cast<const uint32_t*>(&h);
+  }
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// Eight elements of chunk `c` of this thread: consecutive ones where the arrays allow 16-byte
+// accesses (VEC), else one in every blockDim.x.
+template <bool VEC>
+__device__ __forceinline__ int column(int c, int e) {
+  return VEC ? (c * (int)blockDim.x + (int)threadIdx.x) * 8 + e : (c * 8 + e) * (int)blockDim.x + (int)threadIdx.x;
+}
+
+template <int TYPE, bool VEC>
+__device__ __forceinline__ void load8(const void* row, int c, int n, float* v) {
+  if (VEC) {
+    const int i = column<true>(c, 0);
+    if (i < n) {
+      if (TYPE == QTEA_TYPE_F32) {
+        const float4* p = reinterpret_cast<const float4*>(static_cast<const float*>(row) + i);
+        const float4 a = p[0], b = p[1];
+        v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
+      } else {
+        unpack8(*reinterpret_cast<const uint4*>(static_cast<const __half*>(row) + i), v);
+      }
+      return;
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const int i = column<false>(c, e);
+      v[e] = i < n ? load1<TYPE>(row, i) : 0.f;
+    }
+    return;
+  }
+#pragma unroll
+  for (int e = 0; e < 8; ++e) v[e] = 0.f;
+}
+
+template <int TYPE, bool VEC>
+__device__ __forceinline__ void store8(void* row, int c, int n, const float* v) {
+  if (VEC) {
+    const int i = column<true>(c, 0);
+    if (i >= n) return;
+    if (TYPE == QTEA_TYPE_F32) {
+      float4* p = reinterpret_cast<float4*>(static_cast<float*>(row) + i);
+      p[0] = make_float4(v[0], v[1], v[2], v[3]);
+      p[1] = make_float4(v[4], v[5], v[6], v[7]);
+    } else {
+      *reinterpret_cast<uint4*>(static_cast<__half*>(row) + i) = pack8(v);
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const int i = column<false>(c, e);
+      if (i < n) {
+        if (TYPE == QTEA_TYPE_F32) static_cast<float*>(row)[i] = v[e];
+        else static_cast<__half*>(row)[i] = __float2half_rn(v[e]);
+      }
+    }
+  }
+}
+
+__device__ __forceinline__ const char* at(const void* p, long long row, long long ld, int type) {
+  return static_cast<const char*>(p) + row * ld * (type == QTEA_TYPE_F32 ? 4 : 2);
+}
+
+// The CTA's sum of one value per thread, to every thread, in a fixed order. `part` holds 32 floats
+// that nothing else uses until the next barrier after this one.
+__device__ __forceinline__ float cta_sum(float v, float* part) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  const int warps = (int)blockDim.x >> 5;
+  if (warps == 1) return v;
+  if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = v;
+  __syncthreads();
+  float s = (int)(threadIdx.x & 31) < warps ? part[threadIdx.x & 31] : 0.f;
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+  return s;
+}
+
+// C chunks of 8 elements per thread: rows up to 8 C blockDim.x columns.
+template <int HT, int YT, int C, bool VEC>
+__global__ void __launch_bounds__(kNormThreads<C>) qtea_norm_kernel(const NormParams p) {
+  __shared__ float part[2][32];
+  const int n = p.n;
+  const float inv_n = 1.f / (float)n;
+  for (int r = blockIdx.x; r < p.n_rows; r += gridDim.x) {
+    float h[C][8];
+    const void* hrow = at(p.h, r, p.h_ld, HT);
+    if (YT != kNone) {
+      float t[C][8];
+      const void* yrow = at(p.y, r, p.y_ld, YT);
+#pragma unroll
+      for (int c = 0; c < C; ++c) load8<YT, VEC>(yrow, c, n, t[c]);
+#pragma unroll
+      for (int c = 0; c < C; ++c) load8<HT, VEC>(hrow, c, n, h[c]);
+      float f = 1.f;
+      if (p.post) {
+        float s = 0.f;
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) s = fmaf(t[c][e], t[c][e], s);
+        f = rsqrtf(cta_sum(s, part[0]) * inv_n + p.eps);
+      }
+#pragma unroll
+      for (int c = 0; c < C; ++c) {
+        float w[8];
+        if (p.post) {
+          load8<QTEA_TYPE_F16, VEC>(p.post, c, n, w);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) t[c][e] = t[c][e] * f * w[e];
+        }
+        if (p.gate) {
+          load8<QTEA_TYPE_F16, VEC>(at(p.gate, r, p.gate_ld, QTEA_TYPE_F16), c, n, w);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) t[c][e] *= w[e];
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) h[c][e] = fmaf(p.res_scale, t[c][e], h[c][e]);
+        store8<HT, VEC>(const_cast<char*>(at(p.h_out, r, p.h_out_ld, HT)), c, n, h[c]);
+      }
+    } else {
+#pragma unroll
+      for (int c = 0; c < C; ++c) load8<HT, VEC>(hrow, c, n, h[c]);
+    }
+    if (p.x) {
+      float s = 0.f;
+#pragma unroll
+      for (int c = 0; c < C; ++c)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) s = fmaf(h[c][e], h[c][e], s);
+      const float f = rsqrtf(cta_sum(s, part[1]) * inv_n + p.eps);
+#pragma unroll
+      for (int c = 0; c < C; ++c) {
+        float w[8];
+        load8<QTEA_TYPE_F16, VEC>(p.weight, c, n, w);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) h[c][e] = h[c][e] * f * w[e];
+        store8<QTEA_TYPE_F16, VEC>(p.x + r * p.x_ld, c, n, h[c]);
+      }
+    }
+    if (gridDim.x < p.n_rows) __syncthreads();  // the sums' places are used again by the next row
+  }
+}
+
+// Rows longer than the registers hold: the row is read again from memory after each sum. h' goes to
+// h_out, and is formed a second time (from h and y, which h_out may overwrite: each thread reads and
+// writes its own elements only) for x.
+template <int HT, int YT>
+__global__ void __launch_bounds__(1024) qtea_norm_long_kernel(const NormParams p) {
+  __shared__ float part[2][32];
+  const float inv_n = 1.f / (float)p.n;
+  for (int r = blockIdx.x; r < p.n_rows; r += gridDim.x) {
+    const void* hrow = at(p.h, r, p.h_ld, HT);
+    const void* yrow = YT != kNone ? at(p.y, r, p.y_ld, YT) : nullptr;
+    const __half* gate = p.gate ? p.gate + r * p.gate_ld : nullptr;
+    float f = 1.f;
+    if (YT != kNone && p.post) {
+      float s = 0.f;
+      for (int i = threadIdx.x; i < p.n; i += blockDim.x) {
+        const float t = load1<YT>(yrow, i);
+        s = fmaf(t, t, s);
+      }
+      f = rsqrtf(cta_sum(s, part[0]) * inv_n + p.eps);
+    }
+    auto updated = [&](int i) {
+      float v = load1<HT>(hrow, i);
+      if (YT != kNone) {
+        float t = load1<YT>(yrow, i);
+        if (p.post) t = t * f * __half2float(p.post[i]);
+        if (gate) t *= __half2float(gate[i]);
+        v = fmaf(p.res_scale, t, v);
+      }
+      return v;
+    };
+    float g = 0.f;
+    if (p.x) {
+      float s = 0.f;
+      for (int i = threadIdx.x; i < p.n; i += blockDim.x) {
+        const float v = updated(i);
+        s = fmaf(v, v, s);
+      }
+      g = rsqrtf(cta_sum(s, part[1]) * inv_n + p.eps);
+    }
+    for (int i = threadIdx.x; i < p.n; i += blockDim.x) {
+      const float v = updated(i);
+      if (YT != kNone) {
+        void* o = const_cast<char*>(at(p.h_out, r, p.h_out_ld, HT));
+        if (HT == QTEA_TYPE_F32) static_cast<float*>(o)[i] = v;
+        else static_cast<__half*>(o)[i] = __float2half_rn(v);
+      }
+      if (p.x) p.x[r * p.x_ld + i] = __float2half_rn(v * g * __half2float(p.weight[i]));
+    }
+    __syncthreads();
+  }
+}
+
+template <int HT, int YT>
+void launch_types(const NormParams& p, bool vec, cudaStream_t st) {
+  const int grid = std::min(p.n_rows, 1 << 20);
+  const int per8 = (p.n + 7) / 8;  // chunks of eight in a row
+  // One chunk a thread where the rows are few (the shortest chain of loads); four where there are
+  // enough rows for every SM to hold several, or where 1024 threads do not cover the row.
+  const bool wide = per8 > 1024 || (p.n_rows > 4 * 152 && per8 > 128);
+  const int threads = std::max(32, (((wide ? (per8 + 3) / 4 : per8) + 31) / 32) * 32);
+  if (per8 > 4 * 512) {
+    qtea_norm_long_kernel<HT, YT><<<grid, 1024, 0, st>>>(p);
+  } else if (wide) {
+    if (vec) qtea_norm_kernel<HT, YT, 4, true><<<grid, threads, 0, st>>>(p);
+    else qtea_norm_kernel<HT, YT, 4, false><<<grid, threads, 0, st>>>(p);
+  } else {
+    if (vec) qtea_norm_kernel<HT, YT, 1, true><<<grid, threads, 0, st>>>(p);
+    else qtea_norm_kernel<HT, YT, 1, false><<<grid, threads, 0, st>>>(p);
+  }
+}
+
+bool multiple(const void* p, long long ld, int elem, int bytes) {
+  return !p || (reinterpret_cast<uintptr_t>(p) % bytes == 0 && ld * elem % bytes == 0);
+}
+
+}  // namespace
+}  // namespace qtea
+
+using namespace qtea;
+
+extern "C" int qtea_norm(const qtea_norm_args* a, qtea_stream_t stream) {
+  if (!a || a->n_rows < 0 || a->n_cols < 1 || a->n_cols > (1 << 20)) return QTEA_ERR_INVALID_ARG;
+  const auto type_ok = [](int t) { return t == QTEA_TYPE_F32 || t == QTEA_TYPE_F16; };
+  const auto size = [](int t) { return t == QTEA_TYPE_F32 ? 4 : 2; };
+  if (!type_ok(a->h_type) || (a->y && !type_ok(a->y_type))) return QTEA_ERR_INVALID_ARG;
+  if (a->n_rows == 0) return QTEA_OK;
+  const long long n = a->n_cols;
+  const int hs = size(a->h_type), ys = size(a->y_type);
+  if (!a->h || a->h_ld < n || !multiple(a->h, 0, 1, hs)) return QTEA_ERR_INVALID_ARG;
+  if (a->y && (a->y_ld < n || !multiple(a->y, 0, 1, ys) || !a->h_out || a->h_out_ld < n || !multiple(a->h_out, 0, 1, hs)))
+    return QTEA_ERR_INVALID_ARG;
+  if (!a->y && (!a->x || a->post_weight || a->gate)) return QTEA_ERR_INVALID_ARG;
+  if (a->x && (!a->weight || a->x_ld < n)) return QTEA_ERR_INVALID_ARG;
+  if (a->gate && a->gate_ld != 0 && a->gate_ld < n) return QTEA_ERR_INVALID_ARG;
+  for (const void* q : {(const void*)a->post_weight, (const void*)a->gate, (const void*)a->weight, (const void*)a->x})
+    if (!multiple(q, 0, 1, 2)) return QTEA_ERR_INVALID_ARG;
+
+  NormParams p;
+  p.h = a->h;
+  p.y = a->y;
+  p.post = reinterpret_cast<const __half*>(a->post_weight);
+  p.gate = reinterpret_cast<const __half*>(a->gate);
+  p.weight = reinterpret_cast<const __half*>(a->weight);
+  p.h_out = a->h_out;
+  p.x = reinterpret_cast<__half*>(a->x);
+  p.h_ld = a->h_ld, p.y_ld = a->y_ld, p.gate_ld = a->gate_ld, p.h_out_ld = a->h_out_ld, p.x_ld = a->x_ld;
+  p.n_rows = a->n_rows, p.n = a->n_cols;
+  p.res_scale = a->res_scale, p.eps = a->eps;
+  const bool vec = n % 8 == 0 && multiple(p.h, p.h_ld, hs, 16) && multiple(p.y, p.y_ld, ys, 16) &&
+                   multiple(p.post, 0, 2, 16) && multiple(p.gate, p.gate_ld, 2, 16) && multiple(p.weight, 0, 2, 16) &&
+                   (!p.y || multiple(p.h_out, p.h_out_ld, hs, 16)) && multiple(p.x, p.x_ld, 2, 16);
+  cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+  const int y = a->y ? a->y_type : kNone;
+  if (a->h_type == QTEA_TYPE_F32) {
+    if (y == kNone) launch_types<QTEA_TYPE_F32, kNone>(p, vec, st);
+    else if (y == QTEA_TYPE_F32) launch_types<QTEA_TYPE_F32, QTEA_TYPE_F32>(p, vec, st);
+    else launch_types<QTEA_TYPE_F32, QTEA_TYPE_F16>(p, vec, st);
+  } else {
+    if (y == kNone) launch_types<QTEA_TYPE_F16, kNone>(p, vec, st);
+    else if (y == QTEA_TYPE_F32) launch_types<QTEA_TYPE_F16, QTEA_TYPE_F32>(p, vec, st);
+    else launch_types<QTEA_TYPE_F16, QTEA_TYPE_F16>(p, vec, st);
+  }
+  if (cudaGetLastError() != cudaSuccess) return QTEA_ERR_CUDA;
+  return QTEA_OK;
+}

@@ -1,0 +1,391 @@
+"""Binding of the operators around the GEMVs of a decoder layer: the paged key/value cache, the
+attention over it, and the norms around a block (the second part of ``include/qtea.h``).
+
+The functions have the C entry points' names. They sit in a decode loop where a call takes a few
+microseconds, so what does not change between calls is checked and laid out once, in a ``KVCache``
+and a ``KVBatch``; a call then checks its own tensors only.
+"""
+from __future__ import annotations
+
+import ctypes
+
+QTEA_TYPE_F32 = 0
+QTEA_TYPE_F16 = 1
+QTEA_KV_F16 = 0
+QTEA_KV_FP8 = 1
+QTEA_KV_FP4 = 2
+
+_P, _I, _L = ctypes.c_void_p, ctypes.c_int, ctypes.c_longlong
+
+
+class _Batch(ctypes.Structure):
+    _fields_ = [("q_start", _P), ("ctx_len", _P), ("pages", _P), ("n_seqs", _I), ("max_pages", _I), ("n_tokens", _I),
+                ("max_q_len", _I)]
+
+
+class _Append(ctypes.Structure):
+    _fields_ = [("q", _P), ("k", _P), ("v", _P), ("q_ld", _L), ("k_ld", _L), ("v_ld", _L), ("type", _I),
+                ("n_q_heads", _I), ("cos", _P), ("sin", _P), ("n_positions", _I), ("q_norm", _P), ("k_norm", _P),
+                ("eps", ctypes.c_float), ("q_out", _P)]
+
+
+class _Norm(ctypes.Structure):
+    _fields_ = [("h", _P), ("y", _P), ("post_weight", _P), ("gate", _P), ("weight", _P), ("h_out", _P), ("x", _P),
+                ("h_ld", _L), ("y_ld", _L), ("gate_ld", _L), ("h_out_ld", _L), ("x_ld", _L), ("h_type", _I),
+                ("y_type", _I), ("n_rows", _I), ("n_cols", _I), ("res_scale", ctypes.c_float), ("eps", ctypes.c_float)]
+
+
+def _bind(lib):
+    """Argument types of this part's entry points."""
+    S, F = ctypes.c_size_t, ctypes.c_float
+    lib.qtea_kv_create.restype = _I
+    lib.qtea_kv_create.argtypes = [_P, _P, _P, _P, _I, _I, _I, _I, _I, ctypes.POINTER(_P)]
+    lib.qtea_kv_free.restype = None
+    lib.qtea_kv_free.argtypes = [_P]
+    lib.qtea_kv_append.restype = _I
+    lib.qtea_kv_append.argtypes = [_P, _P, _P, _P]
+    lib.qtea_kv_read.restype = _I
+    lib.qtea_kv_read.argtypes = [_P, _P, _P, _I, _P, _P, _P]
+    lib.qtea_attention.restype = _I
+    lib.qtea_attention.argtypes = [_P, _P, _P, _L, _I, F, _I, _P, _L, _P, _P, S, _P]
+    lib.qtea_attention_workspace.restype = _I
+    lib.qtea_attention_workspace.argtypes = [ctypes.POINTER(S)]
+    lib.qtea_attention_status.restype = _I
+    lib.qtea_attention_status.argtypes = [_P, S, _P]
+    lib.qtea_norm.restype = _I
+    lib.qtea_norm.argtypes = [_P, _P]
+
+
+def _package():
+    import paper_2609_00224_gb300 as qt
+    return qt
+
+
+_state = {}
+
+
+def _lib():
+    lib = _state.get("lib")
+    if lib is None:
+        import torch
+        lib = _package().load()
+        _state.update(lib=lib, raw_stream=torch._C._cuda_getCurrentRawStream, f16=torch.float16, f32=torch.float32)
+    return lib
+
+
+def _stream_of(stream, device):
+    if stream is None:
+        return _state["raw_stream"](device)
+    return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
+
+
+def _fail(rc, where):
+    raise _package().QteaError(rc, where)
+
+
+def _array(t, dtypes, name, shape):
+    """A contiguous CUDA tensor of one of these types and this shape: its pointer."""
+    if not t.is_cuda:
+        raise TypeError(f"{name} must be a CUDA tensor")
+    if t.dtype not in dtypes:
+        raise TypeError(f"{name} has dtype {t.dtype}, expected one of {dtypes}")
+    if tuple(t.shape) != shape or not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous with shape {shape}, got {tuple(t.shape)}")
+    return t.data_ptr()
+
+
+def _rows(t, dtype, name, rows, cols):
+    """A tensor of `rows` rows of `cols` elements in all, dense within a row: its pointer and row stride."""
+    if t.dtype is not dtype:
+        raise TypeError(f"{name} has dtype {t.dtype}, expected {dtype}")
+    if not t.is_cuda:
+        raise TypeError(f"{name} must be a CUDA tensor")
+    if t.shape[0] != rows or t.numel() != rows * cols:
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {rows} rows of {cols} elements")
+    if t.is_contiguous():
+        return t.data_ptr(), cols
+    st = t.stride()
+    inner, n = 1, t.dim()
+    for d in range(n - 1, 0, -1):
+        if t.shape[d] != 1 and st[d] != inner:
+            raise ValueError(f"{name} must be dense within a row")
+        inner *= t.shape[d]
+    # one row has no next one: its stride is free
+    return t.data_ptr(), st[0] if rows > 1 else cols
+
+
+class KVCache:
+    """A paged key/value cache in the caller's tensors.
+
+    k_pages, v_pages: [n_pages][kv heads][page_size][head_dim] fp16, or uint8 (FP8: also
+    float8_e4m3fn) codes, with head_dim / 2 bytes a row for FP4; k_scale, v_scale: uint8
+    [n_pages][kv heads][page_size][head_dim / 32] for FP8 and FP4.
+    """
+
+    def __init__(self, k_pages, v_pages, k_scale=None, v_scale=None, fmt: int = QTEA_KV_F16):
+        import torch
+        lib = _lib()
+        self._h = None
+        if k_pages.dim() != 4:
+            raise ValueError("pages must be [n_pages][kv heads][page_size][head_dim]")
+        if fmt not in (QTEA_KV_F16, QTEA_KV_FP8, QTEA_KV_FP4):
+            raise ValueError(f"unknown cache format {fmt}")
+        n, heads, page, row = k_pages.shape
+        dim = row * 2 if fmt == QTEA_KV_FP4 else row
+        types = {QTEA_KV_F16: (torch.float16,), QTEA_KV_FP8: (torch.uint8, torch.float8_e4m3fn),
+                 QTEA_KV_FP4: (torch.uint8,)}[fmt]
+        kp = _array(k_pages, types, "k_pages", (n, heads, page, row))
+        vp = _array(v_pages, types, "v_pages", (n, heads, page, row))
+        ks = vs = None
+        if fmt != QTEA_KV_F16:
+            if k_scale is None or v_scale is None:
+                raise ValueError("this cache format needs k_scale and v_scale")
+            ks = _array(k_scale, (torch.uint8,), "k_scale", (n, heads, page, dim // 32))
+            vs = _array(v_scale, (torch.uint8,), "v_scale", (n, heads, page, dim // 32))
+        out = ctypes.c_void_p()
+        rc = lib.qtea_kv_create(kp, vp, ks, vs, n, page, heads, dim, fmt, ctypes.byref(out))
+        if rc:
+            _fail(rc, "qtea_kv_create")
+        self._h = out.value
+        self._free = lib.qtea_kv_free
+        self.k_pages, self.v_pages, self.k_scale, self.v_scale = k_pages, v_pages, k_scale, v_scale
+        self.format, self.n_pages, self.page_size, self.n_kv_heads, self.head_dim = fmt, n, page, heads, dim
+        self.device = k_pages.device.index
+
+    @classmethod
+    def empty(cls, n_pages: int, page_size: int, n_kv_heads: int, head_dim: int, fmt: int = QTEA_KV_F16,
+              device="cuda") -> "KVCache":
+        """A cache in new tensors."""
+        import torch
+        row = head_dim // 2 if fmt == QTEA_KV_FP4 else head_dim
+        dtype = torch.float16 if fmt == QTEA_KV_F16 else torch.uint8
+        pages = [torch.empty((n_pages, n_kv_heads, page_size, row), dtype=dtype, device=device) for _ in range(2)]
+        scales = [None, None]
+        if fmt != QTEA_KV_F16:
+            scales = [torch.empty((n_pages, n_kv_heads, page_size, head_dim // 32), dtype=torch.uint8, device=device)
+                      for _ in range(2)]
+        return cls(*pages, *scales, fmt=fmt)
+
+    @property
+    def handle(self):
+        if self._h is None:
+            raise ValueError("cache was freed")
+        return self._h
+
+    def free(self):
+        if self._h is not None:
+            self._free(self._h)
+            self._h = None
+
+    def __del__(self):
+        try:
+            self.free()
+        except Exception:
+            pass
+
+
+class KVBatch:
+    """The sequences of a call (qtea_kv_batch): q_start int32 [n_seqs + 1], ctx_len int32 [n_seqs],
+    pages int32 [n_seqs][max_pages]. The tensors are kept; their contents may change between calls."""
+
+    def __init__(self, q_start, ctx_len, pages, n_tokens: int, max_q_len: int):
+        import torch
+        if pages.dim() != 2:
+            raise ValueError("pages must be [n_seqs][max_pages]")
+        n, most = pages.shape
+        i32 = (torch.int32,)
+        self._c = _Batch(_array(q_start, i32, "q_start", (n + 1,)), _array(ctx_len, i32, "ctx_len", (n,)),
+                         _array(pages, i32, "pages", (n, most)), n, most, int(n_tokens), int(max_q_len))
+        self._ref = ctypes.addressof(self._c)
+        self.q_start, self.ctx_len, self.pages = q_start, ctx_len, pages
+        self.n_tokens, self.max_q_len = int(n_tokens), int(max_q_len)
+
+
+def qtea_kv_append(cache: KVCache, batch: KVBatch, k, v, q=None, cos=None, sin=None, q_norm=None, k_norm=None,
+                   eps: float = 1e-6, q_out=None, stream=None):
+    """Write the batch's new tokens into the cache; with q, returns the prepared queries.
+
+    q, k, v: [n_tokens][heads * head_dim] (or [n_tokens][heads][head_dim]), all fp32 or all fp16, rows
+    may be strided. cos, sin: fp32 [positions][head_dim / 2]. q_norm, k_norm: fp16 [head_dim].
+    q_out: fp16 [n_tokens][q heads][head_dim], made when not given.
+    """
+    import torch
+    lib = _lib()
+    n, dim = batch.n_tokens, cache.head_dim
+    a = _Append()
+    dtype = k.dtype
+    if dtype is not _state["f32"] and dtype is not _state["f16"]:
+        raise TypeError(f"k has dtype {dtype}, expected float32 or float16")
+    a.type = QTEA_TYPE_F32 if dtype is _state["f32"] else QTEA_TYPE_F16
+    a.k, a.k_ld = _rows(k, dtype, "k", n, cache.n_kv_heads * dim)
+    a.v, a.v_ld = _rows(v, dtype, "v", n, cache.n_kv_heads * dim)
+    if q is not None:
+        if n and q.numel() % (n * dim):
+            raise ValueError(f"q has shape {tuple(q.shape)}, not whole heads of {dim}")
+        heads = q.numel() // (n * dim) if n else 1
+        a.q, a.q_ld = _rows(q, dtype, "q", n, heads * dim)
+        a.n_q_heads = heads
+        if q_out is None:
+            q_out = torch.empty((n, heads, dim), dtype=torch.float16, device=q.device)
+        a.q_out = _array(q_out, (_state["f16"],), "q_out", (n, heads, dim))
+    if cos is not None:
+        if sin is None:
+            raise ValueError("cos and sin come together")
+        a.n_positions = cos.shape[0]
+        if a.n_positions < 1:  # its pointer would be NULL: no rotation
+            _fail(1, "qtea_kv_append")
+        a.cos = _array(cos, (_state["f32"],), "cos", (a.n_positions, dim // 2))
+        a.sin = _array(sin, (_state["f32"],), "sin", (a.n_positions, dim // 2))
+    elif sin is not None:
+        raise ValueError("cos and sin come together")
+    if q_norm is not None:
+        a.q_norm = _array(q_norm, (_state["f16"],), "q_norm", (dim,))
+    if k_norm is not None:
+        a.k_norm = _array(k_norm, (_state["f16"],), "k_norm", (dim,))
+    a.eps = eps
+    rc = lib.qtea_kv_append(cache.handle, batch._ref, ctypes.addressof(a), _stream_of(stream, cache.device))
+    if rc:
+        _fail(rc, "qtea_kv_append")
+    return q_out if q is not None else None
+
+
+def qtea_kv_read(cache: KVCache, batch: KVBatch, row_start, n_rows=None, k_out=None, v_out=None, stream=None):
+    """The sequences' cached rows as fp16 [n_rows][kv heads][head_dim]: (k, v). Sequence s takes the
+    rows from row_start[s] (int32 [n_seqs + 1], on the device); n_rows is needed when neither output
+    is given."""
+    import torch
+    lib = _lib()
+    if n_rows is None:
+        if k_out is None and v_out is None:
+            raise ValueError("n_rows is needed to make the outputs")
+        n_rows = (k_out if k_out is not None else v_out).shape[0]
+    shape = (int(n_rows), cache.n_kv_heads, cache.head_dim)
+    if k_out is None and v_out is None:
+        k_out, v_out = (torch.empty(shape, dtype=torch.float16, device=cache.k_pages.device) for _ in range(2))
+    f16 = (_state["f16"],)
+    rc = lib.qtea_kv_read(cache.handle, batch._ref,
+                          _array(row_start, (torch.int32,), "row_start", (batch._c.n_seqs + 1,)), shape[0],
+                          _array(k_out, f16, "k_out", shape) if k_out is not None else None,
+                          _array(v_out, f16, "v_out", shape) if v_out is not None else None,
+                          _stream_of(stream, cache.device))
+    if rc:
+        _fail(rc, "qtea_kv_read")
+    return k_out, v_out
+
+
+_workspaces = {}
+
+
+def attention_workspace(device=None, stream=None):
+    """The workspace that qtea_attention uses on a stream when it is given none (one per device and
+    stream, zeroed when it is made and kept: calls on one stream are in order)."""
+    import torch
+    lib = _lib()
+    device = torch.cuda.current_device() if device is None else device
+    raw = _stream_of(stream, device)
+    ws = _workspaces.get((device, raw))
+    if ws is None:
+        n = ctypes.c_size_t()
+        with torch.cuda.device(device):
+            rc = lib.qtea_attention_workspace(ctypes.byref(n))
+            if rc:
+                _fail(rc, "qtea_attention_workspace")
+            ws = torch.zeros(n.value, dtype=torch.uint8, device=f"cuda:{device}")
+            if not torch.cuda.is_current_stream_capturing():
+                torch.cuda.current_stream().synchronize()  # the call may be for another stream
+        _workspaces[(device, raw)] = ws
+    return ws
+
+
+def qtea_attention(cache: KVCache, batch: KVBatch, q, scale=None, window: int = 0, out=None, lse=None, workspace=None,
+                   stream=None):
+    """Attention of the batch's new tokens over the cache: fp16 [n_tokens][q heads][head_dim].
+
+    q: fp16 of that shape (rows may be strided); scale: head_dim ** -0.5 by default; window: a token
+    sees at most that many positions, itself among them (0: all). lse: fp32 [n_tokens][q heads], written when given.
+    """
+    import torch
+    lib = _lib()
+    n, dim = batch.n_tokens, cache.head_dim
+    if q.dim() != 3 or q.shape[2] != dim:
+        raise ValueError(f"q must be [n_tokens][q heads][{dim}], got {tuple(q.shape)}")
+    heads = q.shape[1]
+    q_ptr, q_ld = _rows(q, _state["f16"], "q", n, heads * dim)
+    if out is None:
+        out = torch.empty((n, heads, dim), dtype=torch.float16, device=q.device)
+    o_ptr, o_ld = _rows(out, _state["f16"], "out", n, heads * dim)
+    stream = _stream_of(stream, cache.device)
+    if workspace is None:
+        workspace = _workspaces.get((cache.device, stream))
+        if workspace is None:
+            workspace = attention_workspace(cache.device, stream)
+    rc = lib.qtea_attention(cache.handle, batch._ref, q_ptr, q_ld, heads, dim ** -0.5 if scale is None else scale,
+                            window, o_ptr, o_ld,
+                            None if lse is None else _array(lse, (_state["f32"],), "lse", (n, heads)),
+                            workspace.data_ptr(), workspace.numel() * workspace.element_size(), stream)
+    if rc:
+        _fail(rc, "qtea_attention")
+    return out
+
+
+def qtea_attention_status(workspace, stream=None) -> int:
+    return _lib().qtea_attention_status(workspace.data_ptr(), workspace.numel() * workspace.element_size(),
+                                        _stream_of(stream, workspace.device.index))
+
+
+def _typed_rows(t, name, rows, cols):
+    dtype = t.dtype
+    if dtype is not _state["f32"] and dtype is not _state["f16"]:
+        raise TypeError(f"{name} has dtype {dtype}, expected float32 or float16")
+    p, ld = _rows(t, dtype, name, rows, cols)
+    return p, ld, QTEA_TYPE_F32 if dtype is _state["f32"] else QTEA_TYPE_F16
+
+
+def qtea_norm(h, weight=None, y=None, post_weight=None, gate=None, res_scale: float = 1.0, eps: float = 1e-6,
+              h_out=None, x=None, want_x: bool = True, stream=None):
+    """The norms around a block: h += res_scale * gate * norm(y, post_weight), x = norm(h, weight).
+
+    h: the residual stream [rows][cols], fp32 or fp16, updated in place unless h_out is given; y: the
+    block's output (fp32 or fp16), or None for the norm before a block alone; gate: fp16 [cols] or
+    [rows][cols]; weights: fp16 [cols]. Returns x, fp16 [rows][cols] (None with want_x=False: the last
+    residual of a model, whose norm comes later).
+    """
+    import torch
+    lib = _lib()
+    if h.dim() != 2:
+        raise ValueError("h must be [rows][cols]")
+    n, cols = h.shape
+    f16 = _state["f16"]
+    a = _Norm()
+    a.n_rows, a.n_cols, a.res_scale, a.eps = n, cols, res_scale, eps
+    a.h, a.h_ld, a.h_type = _typed_rows(h, "h", n, cols)
+    if y is not None:
+        a.y, a.y_ld, a.y_type = _typed_rows(y, "y", n, cols)
+        if h_out is None or h_out is h:
+            a.h_out, a.h_out_ld = a.h, a.h_ld
+        else:
+            a.h_out, a.h_out_ld = _rows(h_out, h.dtype, "h_out", n, cols)
+        if post_weight is not None:
+            a.post_weight = _array(post_weight, (f16,), "post_weight", (cols,))
+        if gate is not None:
+            if gate.dim() == 1:
+                a.gate = _array(gate, (f16,), "gate", (cols,))
+            else:
+                a.gate, a.gate_ld = _rows(gate, f16, "gate", n, cols)
+    elif post_weight is not None or gate is not None or h_out is not None:
+        raise ValueError("post_weight, gate and h_out go with y")
+    if want_x:
+        if weight is None:
+            raise ValueError("x needs weight")
+        a.weight = _array(weight, (f16,), "weight", (cols,))
+        if x is None:
+            x = torch.empty((n, cols), dtype=f16, device=h.device)
+        a.x, a.x_ld = _rows(x, f16, "x", n, cols)
+    elif y is None:
+        raise ValueError("nothing to do without y and x")
+    else:
+        x = None
+    rc = lib.qtea_norm(ctypes.addressof(a), _stream_of(stream, h.device.index))
+    if rc:
+        _fail(rc, "qtea_norm")
+    return x
