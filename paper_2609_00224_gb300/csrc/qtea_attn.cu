@@ -29,6 +29,7 @@ namespace qtea {
 namespace {
 
 constexpr int kWarps = 4;
+constexpr int kMaxRows = 32;
 constexpr float kLag = 8.f;
 constexpr int kRowsGrid = 320;  // the weights of that many parts fit the rings
 constexpr float kNegInf = -INFINITY;
@@ -489,7 +490,7 @@ __global__ void __launch_bounds__(kWarps * 32, 2)
       const int tok = it.seq.q0 + i0 + r / p.group, h = it.head * p.group + r % p.group;
       if (p.lse) p.lse[(long long)tok * p.q_heads + h] = sum > 0.f ? (top + log2f(sum)) * 0.6931471805599453f : sum == 0.f ? kNegInf : sum;
     };
-    const size_t slot_floats = (size_t)D * R + 2 * R;
+    const size_t slot_floats = (size_t)D * R + 2 * R;  // a multiple of four
     float* slot = p.slots + (2 * (size_t)blockIdx.x + ((int)blockIdx.x == c0 ? 1 : 0)) * slot_floats;
     for (int e = threadIdx.x; e < D * R; e += kWarps * 32) {
       const int r = e % R, d = e / R;
@@ -519,33 +520,44 @@ __global__ void __launch_bounds__(kWarps * 32, 2)
       __syncthreads();
       if (is_last) {
         __threadfence();
-        // the parts' weights, [part][row], then their sum in the parts' order
+        // The parts' weights, [part][row] in shared memory, then the weighted
+        // sum in the parts' order: four rows of one column a thread, 16 bytes a part, eight parts'
+        // loads in flight.
         const int parts = c1 - c0 + 1;
-        auto part = [&](int i) {
-          return p.slots + (2 * (size_t)(c0 + i) + (i == 0 ? 1 : 0)) * slot_floats;
-        };
+        auto part = [&](int i) { return p.slots + (2 * (size_t)(c0 + i) + (i == 0 ? 1 : 0)) * slot_floats; };
         for (int e = threadIdx.x; e < parts * R; e += kWarps * 32) join[e] = __ldcg(part(e / R) + D * R + e % R);
         __syncthreads();
-        if (threadIdx.x < R) {
-          const int r = threadIdx.x;
+        for (int r = warp; r < R; r += kWarps) {
           float top = kNegInf, sum = 0.f;
-          for (int i = 0; i < parts; ++i) top = fmaxf(top, join[i * R + r]);
-          for (int i = 0; i < parts; ++i) {
+          for (int i = lane; i < parts; i += 32) top = fmaxf(top, join[i * R + r]);
+#pragma unroll
+          for (int w = 16; w > 0; w >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, w));
+          for (int i = lane; i < parts; i += 32) {
             const float f = top == kNegInf ? 0.f : ex2(join[i * R + r] - top);
             join[i * R + r] = f;
             sum = fmaf(__ldcg(part(i) + D * R + R + r), f, sum);
           }
-          joined_l[r] = sum;
-          if (r < rows) write_lse(r, top, sum);
+#pragma unroll
+          for (int w = 16; w > 0; w >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, w);
+          if (lane == 0) {
+            joined_l[r] = sum;
+            if (r < rows) write_lse(r, top, sum);
+          }
         }
         __syncthreads();
-        for (int e = threadIdx.x; e < D * R; e += kWarps * 32) {
+        for (int e = 4 * threadIdx.x; e < D * R; e += 4 * kWarps * 32) {
           const int r = e % R, d = e / R;
-          if (r >= rows) continue;
-          float v = 0.f;
+          float v[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 8
-          for (int i = 0; i < parts; ++i) v = fmaf(__ldcg(part(i) + e), join[i * R + r], v);
-          write_out(r, d, joined_l[r] == 0.f ? 0.f : v / joined_l[r]);
+          for (int i = 0; i < parts; ++i) {
+            const float4 x = __ldcg(reinterpret_cast<const float4*>(part(i) + e));
+            const float4 f = *reinterpret_cast<const float4*>(join + i * R + r);
+            v[0] = fmaf(x.x, f.x, v[0]), v[1] = fmaf(x.y, f.y, v[1]);
+            v[2] = fmaf(x.z, f.z, v[2]), v[3] = fmaf(x.w, f.w, v[3]);
+          }
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            if (r + k < rows) write_out(r + k, d, joined_l[r + k] == 0.f ? 0.f : v[k] / joined_l[r + k]);
         }
       }
     }
@@ -580,8 +592,6 @@ cudaError_t launch_dim(const qtea_kv* kv, const AttnParams& p, int nt, int grid,
   return kv->view.dim == 128 ? launch_nt<FMT, 128>(kv, p, nt, grid, st) : launch_nt<FMT, 64>(kv, p, nt, grid, st);
 }
 
-constexpr int kMaxRows = 32;
-
 }  // namespace
 
 int attn_rows_grid(int sm_count) { return std::min(2 * sm_count, kRowsGrid); }
@@ -610,7 +620,7 @@ namespace {
 bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
 
 size_t workspace_bytes_for(int sm_count) {
-  return kAttnHeaderBytes + 2 * sizeof(float) * attn_rows_floats(sm_count);
+  return kAttnHeaderBytes + 2 * sizeof(float) * std::max(attn_rows_floats(sm_count), attn_chunk_floats(sm_count));
 }
 }  // namespace
 
@@ -658,7 +668,8 @@ int qtea_attention(const qtea_kv* kv, const qtea_kv_batch* batch, const uint16_t
   p.counters = reinterpret_cast<unsigned*>(workspace) + 64;
   p.slots = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + kAttnHeaderBytes);
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
-  if (launch_attn_rows(kv, p, st) != cudaSuccess) {
+  const bool few = (long long)p.group * p.b.max_q <= kMaxRows;
+  if ((few ? launch_attn_rows(kv, p, st) : launch_attn_chunk(kv, p, st)) != cudaSuccess) {
     cudaGetLastError();
     return QTEA_ERR_CUDA;
   }

@@ -34,6 +34,8 @@ struct AttnParams {
   float* slots;     // [grid][2] partial results
 };
 
+cudaError_t launch_attn_chunk(const qtea_kv* kv, const AttnParams& p, cudaStream_t st);
+size_t attn_chunk_floats(int sm_count);  // of one partial result for each CTA
 cudaError_t launch_attn_rows(const qtea_kv* kv, const AttnParams& p, cudaStream_t st);
 size_t attn_rows_floats(int sm_count);  // of one partial result for each CTA
 

@@ -1,0 +1,882 @@
+// Attention of many query rows per cache head over the paged cache (chunks, prompts) on the fifth-
+// generation tensor cores.
+//
+// With R query rows sharing a cache head, a unit of 128 keys takes 4 * 128 * 128 * D operations per 128
+// rows: at D = 128 two tcgen05.mma of about 512 clocks each, against 16384 exponentials. The form follows
+// from keeping the tensor pipe fed while those are computed:
+//  * two softmax groups of 128 threads, one thread per query row (a lane of TMEM), each with its own
+//    S and O accumulators (S0, S1, O0, O1 fill the 512 columns). While one group turns its S into
+//    weights, the tensor cores work for the other. With more than 128 rows in an item the groups take a
+//    tile of rows each over the same keys; with fewer they take every second unit of keys of the
+//    same rows, and join their halves at the end;
+//  * the weights go back to TMEM over S, as fp16, and are the second product's A operand from there;
+//  * over an fp16 cache, a row's weights are formed against the reference that it has, its maximum in
+//    the first unit, without looking for this unit's maximum first: that is known when the weights
+//    are, and only where a weight passes 2^15, near fp16's end, are they formed again against a new reference
+//    and the accumulator rescaled. Until then a thread holds 64 registers of weights; over a
+//    quantised cache the converting warps need those registers, so there the maximum is looked for
+//    first, in a second reading of S, and the reference follows it by at most 2^8;
+//  * one warp issues every product, one warp every copy; keys and values are boxes of 16 tokens
+//    swizzled on the way into shared memory. K is the second operand K-major, V is taken MN-major, so
+//    neither is transposed. Quantised rows are copied as they are into a ring of their own, and four
+//    warps write them as fp16 (exactly) in the same swizzled form.
+// The tensor pipe executes one thread's products in order, which replaces most barriers: when S of
+// step j+1 has been signalled, O of step j is complete and its weights' columns are free.
+#include <cudaTypedefs.h>
+
+#include <algorithm>
+#include <cmath>
+#include <cstring>
+
+#include "qtea_attn.h"
+
+namespace qtea {
+namespace {
+
+constexpr float kTop = 15.f;  // weights up to 2^15 are within fp16
+constexpr float kLag = 8.f;
+constexpr float kNegInf = -INFINITY;
+constexpr int kUnit = 128;  // keys
+constexpr int kRowsTile = 128;
+
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+// ---------------------------------------------------------------------------------- tcgen05 wrappers
+
+__device__ __forceinline__ void tmem_alloc(uint32_t dst, uint32_t cols) {
+  asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(dst), "r"(cols) : "memory");
+  asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void tmem_free(uint32_t base, uint32_t cols) {
+  asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(base), "r"(cols) : "memory");
+}
+// D[tmem] (+)= A[shared] * B[shared]
+__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{ .reg .pred p; setp.ne.b32 p, %4, 0;\n"
+      "  tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p; }" ::"r"(d),
+      "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+// D[tmem] (+)= A[tmem] * B[shared]
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{ .reg .pred p; setp.ne.b32 p, %4, 0;\n"
+      "  tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p; }" ::"r"(d),
+      "r"(a), "l"(b), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+// The barrier is arrived at once when everything this thread has issued is complete.
+__device__ __forceinline__ void mma_commit(uint32_t bar) {
+  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void tmem_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tmem_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+#define QTEA_R8(r, i) "=r"(r[i]), "=r"(r[i + 1]), "=r"(r[i + 2]), "=r"(r[i + 3]), "=r"(r[i + 4]), "=r"(r[i + 5]), "=r"(r[i + 6]), "=r"(r[i + 7])
+#define QTEA_W8(r, i) "r"(r[i]), "r"(r[i + 1]), "r"(r[i + 2]), "r"(r[i + 3]), "r"(r[i + 4]), "r"(r[i + 5]), "r"(r[i + 6]), "r"(r[i + 7])
+
+// 32 consecutive columns of this thread's lane
+__device__ __forceinline__ void tmem_ld32(uint32_t* r, uint32_t addr) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+      : QTEA_R8(r, 0), QTEA_R8(r, 8), QTEA_R8(r, 16), QTEA_R8(r, 24)
+      : "r"(addr)
+      : "memory");
+}
+__device__ __forceinline__ void tmem_st32(uint32_t addr, const uint32_t* r) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, "
+      "%15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31};" ::QTEA_W8(r, 0),
+      QTEA_W8(r, 8), QTEA_W8(r, 16), QTEA_W8(r, 24), "r"(addr)
+      : "memory");
+}
+
+__device__ __forceinline__ void tmem_ld16(uint32_t* r, uint32_t addr) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, "
+      "[%16];"
+      : QTEA_R8(r, 0), QTEA_R8(r, 8)
+      : "r"(addr)
+      : "memory");
+}
+__device__ __forceinline__ void tmem_st16(uint32_t addr, const uint32_t* r) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, "
+      "%15};" ::QTEA_W8(r, 0),
+      QTEA_W8(r, 8), "r"(addr)
+      : "memory");
+}
+
+__device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::
+          "r"(dst),
+      "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(bar)
+      : "memory");
+}
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst),
+               "l"(reinterpret_cast<uint64_t>(src)), "r"(bytes), "r"(bar)
+               : "memory");
+}
+__device__ __forceinline__ void sts128(uint32_t a, uint4 v) {
+  asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(a), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+}
+__device__ __forceinline__ uint4 lds128(uint32_t a) {
+  uint4 v;
+  asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a) : "memory");
+  return v;
+}
+__device__ __forceinline__ uint32_t lds8(uint32_t a) {
+  uint32_t r;
+  asm volatile("ld.shared.u8 %0, [%1];" : "=r"(r) : "r"(a) : "memory");
+  return r;
+}
+__device__ __forceinline__ void fence_async_shared() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+template <int ID>
+__device__ __forceinline__ void named_barrier(int threads) {
+  asm volatile("bar.sync %0, %1;" ::"n"(ID), "r"(threads) : "memory");
+}
+template <int N>
+__device__ __forceinline__ void regs_up() {
+  asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N));
+}
+template <int N>
+__device__ __forceinline__ void regs_down() {
+  asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N));
+}
+
+// Two fp32 at a time.
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  float2 d;
+  asm("{ .reg .b64 a, b, c, d; mov.b64 a, {%2, %3}; mov.b64 b, {%4, %5}; mov.b64 c, {%6, %7};\n"
+      "  fma.rn.f32x2 d, a, b, c; mov.b64 {%0, %1}, d; }"
+      : "=f"(d.x), "=f"(d.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+  return d;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  float2 d;
+  asm("{ .reg .b64 a, b, d; mov.b64 a, {%2, %3}; mov.b64 b, {%4, %5};\n"
+      "  add.rn.f32x2 d, a, b; mov.b64 {%0, %1}, d; }"
+      : "=f"(d.x), "=f"(d.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return d;
+}
+
+// Shared-memory operand descriptors, 128-byte swizzle, rows of 128 bytes, 8-row atoms of 1024 bytes.
+// K-major (head_dim contiguous, rows are M or N): the next 8 rows are 1024 bytes on. MN-major
+// (rows are K): the next 8 rows of K are 1024 bytes on, the next 64 of N `lead` bytes.
+__device__ __forceinline__ uint64_t operand(uint32_t addr, uint32_t lead) {
+  return (uint64_t)((addr & 0x3ffffu) >> 4) | (uint64_t)(lead >> 4) << 16 | (uint64_t)(1024u >> 4) << 32 | 1ull << 46 |
+         2ull << 61;
+}
+
+template <int FMT, int D>
+struct Chunk {
+  static constexpr bool kQuant = FMT != QTEA_KV_F16;
+  static constexpr int kParts = D / 64;                       // 64-element columns of a tile
+  static constexpr int kPartBytes = kUnit * 128;              // 16 KB
+  static constexpr int kTileBytes = kParts * kPartBytes;      // K, V or Q of 128 rows
+  static constexpr int kStages = kQuant ? (D == 128 ? 3 : 4) : (D == 128 ? 4 : 8);
+  static constexpr int kRawRow = FMT == QTEA_KV_FP8 ? D : D / 2;  // bytes of a quantised row
+  static constexpr int kScaleRow = D / kKvBlock;
+  static constexpr int kRawBytes = kQuant ? kUnit * (kRawRow + kScaleRow) : 0;
+  static constexpr int kRawStages = kQuant ? (FMT == QTEA_KV_FP8 ? 3 : 6) : 0;
+  static constexpr int kSmem = 2 * kTileBytes + kStages * kTileBytes + kRawStages * kRawBytes + 1024;
+  static constexpr bool kMaxFirst = kQuant;
+  static constexpr int kThreads = kQuant ? 512 : 384;
+  // warps: 0-7 softmax, then (quantised) 8-11 conversion, then the four of the last group
+  static constexpr int kLast = kThreads / 32 - 4;
+  static constexpr int kCopyWarp = kLast, kMmaWarp = kLast + 1, kQWarp = kLast + 2;
+};
+
+struct ChunkShared {
+  long long prefix[kKvMaxSeqs + 1];
+  uint64_t full[8], empty[8];          // stages of K and V
+  uint64_t raw_full[6], raw_empty[6];  // stages of quantised rows
+  uint64_t q_full, q_empty, o_free;
+  uint64_t s_full[2], p_full[2], o_full[2];
+  uint32_t tmem;
+  int is_last;
+  float m1[2][kRowsTile], l1[2][kRowsTile];  // the second group's rows, where both share them; by items' parity
+};
+
+// A step of the copies' order. With two row tiles: K0 V0 K1 V1 ..; with one: K0 K1 V0 K2 V1 ...
+struct Order {
+  int n;     // units
+  bool two;  // two row tiles
+  __device__ __forceinline__ int steps() const { return 2 * n; }
+  __device__ __forceinline__ void at(int i, int* unit, bool* value) const {
+    if (two) {
+      *unit = i >> 1, *value = i & 1;
+    } else if (i == 0) {
+      *unit = 0, *value = false;
+    } else if (i == 2 * n - 1) {
+      *unit = n - 1, *value = true;
+    } else {  // after K0: K1 V0 K2 V1 ...
+      const int k = i - 1;
+      *value = k & 1;
+      *unit = (k & 1) ? k >> 1 : (k >> 1) + 1;
+    }
+  }
+};
+
+struct ChunkParams {
+  AttnParams a;
+  int half_tokens;  // tokens of one row tile
+  bool two;         // items may have two row tiles
+  bool q_map;       // queries come through the tensor map
+  uint32_t q_flip;  // 0x80008000: a negative scale, taken into the queries
+};
+
+// Keys that some row of the item sees: rows of V outside them are set to zero (0 * NaN), for the
+// memory there may hold anything.
+struct Bounds {
+  int lo, hi;
+};
+__device__ __forceinline__ Bounds item_bounds(const AttnParams& p, const AttnItem& it) {
+  const int i0 = it.tile * p.tile_tokens, i1 = min(it.seq.n, i0 + p.tile_tokens) - 1;
+  Bounds b;
+  b.lo = p.window > 0 ? max(0, it.seq.base + i0 - p.window + 1) : 0;
+  b.hi = max(it.seq.base + i1 + 1, 0);
+  return b;
+}
+
+template <int FMT, int D>
+__global__ void __launch_bounds__((Chunk<FMT, D>::kThreads), 1)
+    qtea_attn_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
+                           const __grid_constant__ CUtensorMap map_q, const ChunkParams cp) {
+  using T = Chunk<FMT, D>;
+  extern __shared__ uint8_t smem_raw[];
+  __shared__ ChunkShared sh;
+  const AttnParams& p = cp.a;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t smem = (smem_u32(smem_raw) + 1023u) & ~1023u;
+  const uint32_t q_smem = smem, kv_smem = smem + 2 * T::kTileBytes, raw_smem = kv_smem + T::kStages * T::kTileBytes;
+
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < T::kStages; ++i) {
+      mbar_init(smem_u32(&sh.full[i]), T::kQuant ? 4 : 1);
+      mbar_init(smem_u32(&sh.empty[i]), 1);
+    }
+    for (int i = 0; i < T::kRawStages; ++i) {
+      mbar_init(smem_u32(&sh.raw_full[i]), 1);
+      mbar_init(smem_u32(&sh.raw_empty[i]), 4);
+    }
+    mbar_init(smem_u32(&sh.q_full), 1);
+    mbar_init(smem_u32(&sh.q_empty), 1);
+    mbar_init(smem_u32(&sh.o_free), 8);
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(smem_u32(&sh.s_full[i]), 1);
+      mbar_init(smem_u32(&sh.p_full[i]), 4);
+      mbar_init(smem_u32(&sh.o_full[i]), 1);
+    }
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  attn_prefix(p, sh.prefix);  // ends with a barrier
+  const AttnSplit split = attn_split(p, sh.prefix);
+  if (split.total == 0 || (int)blockIdx.x >= split.ctas) return;
+  const long long begin = split.first(blockIdx.x), end = split.first(blockIdx.x + 1);
+  if (warp == T::kMmaWarp) tmem_alloc(smem_u32(&sh.tmem), 512);
+  tmem_fence_before();
+  __syncthreads();
+  tmem_fence_after();
+  const uint32_t tmem = sh.tmem;
+
+  bool ok = true;  // once a wait has given up, this warp waits no more and runs out
+  auto wait = [&](uint64_t& bar, uint32_t parity) {
+    if (ok) ok = mbar_wait(smem_u32(&bar), parity, p.status);
+    return ok;
+  };
+
+  if (warp >= T::kLast) {
+    
+    if (warp == T::kCopyWarp) {
+      // ------------------------------------------------------------------ copies of keys and values
+      uint32_t stage = 0, phase = 1;  // the first wait of every stage passes
+      for (long long cur = begin; cur < end;) {
+        const AttnItem it = attn_item(p, sh.prefix, cur, end);
+        cur += it.units;
+        const int* pages = p.b.pages + (long long)it.s * p.b.max_pages;
+        const Order order{it.units, cp.two};
+        for (int i = 0; i < order.steps(); ++i) {
+          int unit;
+          bool value;
+          order.at(i, &unit, &value);
+          int row = 0;
+          if (lane < 8) {
+            const int key = (it.unit0 + unit) * kUnit + 16 * lane;
+            const int page = __ldg(pages + min(key >> p.kv.page_shift, p.b.max_pages - 1));
+            row = (min(max(page, 0), p.kv.n_pages - 1) * p.kv.heads + it.head) * p.kv.page_size +
+                  (key & (p.kv.page_size - 1));
+          }
+          if (!wait(T::kQuant ? sh.raw_empty[stage] : sh.empty[stage], phase)) break;
+          const uint32_t bar = smem_u32(T::kQuant ? &sh.raw_full[stage] : &sh.full[stage]);
+          if (lane == 0) mbar_arrive_expect_tx(bar, T::kQuant ? T::kRawBytes : T::kTileBytes);
+          __syncwarp();
+          if (lane < 8) {
+            if (T::kQuant) {
+              const uint32_t dst = raw_smem + stage * T::kRawBytes;
+              bulk_load(dst + lane * 16 * T::kRawRow, (value ? p.kv.v : p.kv.k) + (long long)row * T::kRawRow,
+                        16 * T::kRawRow, bar);
+              bulk_load(dst + kUnit * T::kRawRow + lane * 16 * T::kScaleRow,
+                        (value ? p.kv.vs : p.kv.ks) + (long long)row * T::kScaleRow, 16 * T::kScaleRow, bar);
+            } else {
+              const uint32_t dst = kv_smem + stage * T::kTileBytes + lane * 2048;
+#pragma unroll
+              for (int h = 0; h < T::kParts; ++h)
+                tma_load_2d(dst + h * T::kPartBytes, value ? &map_v : &map_k, h * 128, row, bar);
+            }
+          }
+          if (++stage == (T::kQuant ? T::kRawStages : T::kStages)) stage = 0, phase ^= 1;
+        }
+      }
+    } else if (warp == T::kMmaWarp) {
+      // ------------------------------------------------------------------------------- the products
+      constexpr uint32_t kIdescS = 1u << 4 | (kUnit >> 3) << 17 | (kRowsTile >> 4) << 24;
+      constexpr uint32_t kIdescO = 1u << 4 | 1u << 16 | (D >> 3) << 17 | (kRowsTile >> 4) << 24;
+      uint32_t stage = 0, phase = 0;
+      uint32_t q_phase = 0, o_phase = 1, p_phase[2] = {0, 0};
+      for (long long cur = begin; cur < end;) {
+        const AttnItem it = attn_item(p, sh.prefix, cur, end);
+        cur += it.units;
+        const Bounds in = item_bounds(p, it);
+        const int n = it.units;
+        const bool second = cp.two && it.seq.n - it.tile * p.tile_tokens > cp.half_tokens;
+        wait(sh.q_full, q_phase);
+        q_phase ^= 1;
+        auto release = [&] {  // the stage is free when the products issued so far are complete
+          if (lane == 0) mma_commit(smem_u32(&sh.empty[stage]));
+          __syncwarp();
+          if (++stage == T::kStages) stage = 0, phase ^= 1;
+        };
+        auto scores = [&](int g, int q_tile) {  // S_g = Q K^T
+          tmem_fence_after();
+          if (lane == 0) {
+            const uint32_t qa = q_smem + q_tile * T::kTileBytes, kb = kv_smem + stage * T::kTileBytes;
+#pragma unroll
+            for (int k = 0; k < D / 16; ++k) {
+              const uint32_t at = (k >> 2) * T::kPartBytes + (k & 3) * 32;
+              mma_ss(tmem + g * 128, operand(qa + at, 16), operand(kb + at, 16), kIdescS, k > 0);
+            }
+            mma_commit(smem_u32(&sh.s_full[g]));
+          }
+          __syncwarp();
+        };
+        auto clean = [&](int unit) {  // zeros over the rows of V that nothing sees
+          const int key0 = (it.unit0 + unit) * kUnit;
+          if (T::kQuant || (key0 >= in.lo && key0 + kUnit <= in.hi)) return;
+          const uint32_t base = kv_smem + stage * T::kTileBytes;
+          for (int i = lane; i < kUnit * 8; i += 32) {
+            const int key = key0 + (i >> 3);
+            if (key < in.lo || key >= in.hi)
+#pragma unroll
+              for (int h = 0; h < T::kParts; ++h) sts128(base + h * T::kPartBytes + i * 16, make_uint4(0, 0, 0, 0));
+          }
+          fence_async_shared();
+          __syncwarp();
+        };
+        auto values = [&](int g, bool accumulate, bool last) {  // O_g (+)= P_g V
+          wait(sh.p_full[g], p_phase[g]);
+          p_phase[g] ^= 1;
+          tmem_fence_after();
+          if (lane == 0) {
+            const uint32_t vb = kv_smem + stage * T::kTileBytes;
+#pragma unroll
+            for (int k = 0; k < kUnit / 16; ++k)
+              mma_ts(tmem + 256 + g * 128, tmem + g * 128 + k * 8, operand(vb + k * 2048, T::kPartBytes), kIdescO,
+                     accumulate || k > 0);
+            if (last) mma_commit(smem_u32(&sh.o_full[g]));
+          }
+          __syncwarp();
+        };
+        auto next_full = [&] { wait(sh.full[stage], phase); };
+        auto q_done = [&] {
+          if (lane == 0) mma_commit(smem_u32(&sh.q_empty));
+          __syncwarp();
+        };
+        auto o_ready = [&] {  // the previous item's accumulators have been read
+          wait(sh.o_free, o_phase);
+          o_phase ^= 1;
+        };
+        if (cp.two) {
+          next_full();
+          scores(0, 0);
+          if (second) scores(1, 1);
+          release();
+          if (n == 1) q_done();
+          o_ready();
+          for (int j = 0; j < n && ok; ++j) {
+            // V_j is at `stage`, K_{j+1} at the next one
+            next_full();
+            clean(j);
+            values(0, j > 0, j == n - 1);
+            if (j + 1 < n) {
+              const uint32_t vs = stage, vp = phase;
+              if (++stage == T::kStages) stage = 0, phase ^= 1;
+              next_full();
+              scores(0, 0);
+              stage = vs, phase = vp;
+              if (second) values(1, j > 0, false);
+              release();
+              if (second) scores(1, 1);
+              release();
+              if (j + 2 == n) q_done();
+            } else {
+              if (second) values(1, j > 0, true);
+              release();
+            }
+          }
+        } else {
+          next_full();
+          scores(0, 0);
+          release();
+          if (n > 1) {
+            next_full();
+            scores(1, 0);
+            release();
+          }
+          if (n <= 2) q_done();
+          o_ready();
+          for (int t = 0; t < n && ok; ++t) {
+            next_full();
+            clean(t);
+            values(t & 1, t >= 2, t + 2 >= n);
+            release();
+            if (t + 2 < n) {
+              next_full();
+              scores(t & 1, 0);
+              release();
+              if (t + 3 == n) q_done();
+            }
+          }
+        }
+      }
+    } else if (warp == T::kQWarp) {
+      // ----------------------------------------------------------------------------------- queries
+      uint32_t q_phase = 1;
+      for (long long cur = begin; cur < end;) {
+        const AttnItem it = attn_item(p, sh.prefix, cur, end);
+        cur += it.units;
+        const int i0 = it.tile * p.tile_tokens, tokens = min(it.seq.n - i0, p.tile_tokens);
+        const int tiles = cp.two && tokens > cp.half_tokens ? 2 : 1;
+        if (!wait(sh.q_empty, q_phase)) break;
+        q_phase ^= 1;
+        const uint32_t bar = smem_u32(&sh.q_full);
+        if (cp.q_map) {  // a box is [tokens][query heads of the group][64]: a row tile's rows in order
+          if (lane == 0) {
+            mbar_arrive_expect_tx(bar, tiles * T::kParts * cp.half_tokens * p.group * 128);
+            for (int t = 0; t < tiles; ++t)
+              for (int h = 0; h < T::kParts; ++h)
+                tma_load_3d(q_smem + t * T::kTileBytes + h * T::kPartBytes, &map_q, 64 * h, it.head * p.group,
+                            it.seq.q0 + i0 + t * cp.half_tokens, bar);
+          }
+          __syncwarp();
+        } else {
+          for (int t = 0; t < tiles; ++t) {
+            const int rows = min(tokens - t * cp.half_tokens, cp.half_tokens) * p.group;
+            for (int i = lane; i < rows * (D / 8); i += 32) {
+              const int r = i / (D / 8), ch = i % (D / 8);
+              const uint32_t* from = reinterpret_cast<const uint32_t*>(
+                  p.q + (long long)(it.seq.q0 + i0 + t * cp.half_tokens + r / p.group) * p.q_ld +
+                  (long long)(it.head * p.group + r % p.group) * D + ch * 8);
+              sts128(q_smem + t * T::kTileBytes + (ch >> 3) * T::kPartBytes + r * 128 + (((ch & 7) ^ (r & 7)) << 4),
+                     make_uint4(from[0] ^ cp.q_flip, from[1] ^ cp.q_flip, from[2] ^ cp.q_flip, from[3] ^ cp.q_flip));
+            }
+          }
+          fence_async_shared();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(bar);
+        }
+      }
+    }
+  } else if (T::kQuant && warp >= 8) {
+    // ------------------------------------------------------------------ quantised rows to fp16 tiles
+    const int tid = threadIdx.x - 256;
+    uint32_t stage = 0, phase = 1, raw = 0, raw_phase = 0;
+    for (long long cur = begin; cur < end;) {
+      const AttnItem it = attn_item(p, sh.prefix, cur, end);
+      cur += it.units;
+      const Bounds in = item_bounds(p, it);
+      const Order order{it.units, cp.two};
+      for (int i = 0; i < order.steps() && ok; ++i) {
+        int unit;
+        bool value;
+        order.at(i, &unit, &value);
+        const int key0 = (it.unit0 + unit) * kUnit;
+        wait(sh.raw_full[raw], raw_phase);
+        wait(sh.empty[stage], phase);
+        if (!ok) break;
+        const uint32_t src = raw_smem + raw * T::kRawBytes, sc = src + kUnit * T::kRawRow;
+        const uint32_t dst = kv_smem + stage * T::kTileBytes;
+        const bool edge = value && (key0 < in.lo || key0 + kUnit > in.hi);
+        constexpr int kChunks = T::kRawRow / 16;  // 16-byte pieces of a row
+#pragma unroll 4
+        for (int j = 0; j < kChunks; ++j) {
+          const int at = tid + 128 * j, r = at / kChunks, ch = at % kChunks;
+          const uint4 x = lds128(src + at * 16);
+          const bool zero = edge && (key0 + r < in.lo || key0 + r >= in.hi);
+          if (FMT == QTEA_KV_FP8) {
+            const uint32_t f = scale_bits(lds8(sc + r * T::kScaleRow + (ch >> 1))) * 0x10001u;
+            uint32_t o[8];
+            const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              o[2 * k] = zero ? 0u : hmul2(from_e4m3x2(w[k]), f);
+              o[2 * k + 1] = zero ? 0u : hmul2(from_e4m3x2_hi(w[k]), f);
+            }
+            const uint32_t to = dst + (ch >> 2) * T::kPartBytes + r * 128;
+            const int c0 = (ch & 3) * 2;
+            sts128(to + ((c0 ^ (r & 7)) << 4), make_uint4(o[0], o[1], o[2], o[3]));
+            sts128(to + (((c0 + 1) ^ (r & 7)) << 4), make_uint4(o[4], o[5], o[6], o[7]));
+          } else {
+            const uint32_t f = scale_bits(lds8(sc + r * T::kScaleRow + ch)) * 0x10001u;
+            const uint32_t to = dst + (ch >> 1) * T::kPartBytes + r * 128;
+            const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              uint32_t o[4];
+              from_e2m1x8(w[k], o);
+#pragma unroll
+              for (int e = 0; e < 4; ++e) o[e] = zero ? 0u : hmul2(o[e], f);
+              sts128(to + ((((ch & 1) * 4 + k) ^ (r & 7)) << 4), make_uint4(o[0], o[1], o[2], o[3]));
+            }
+          }
+        }
+        fence_async_shared();
+        __syncwarp();
+        if (lane == 0) {
+          mbar_arrive(smem_u32(&sh.full[stage]));
+          mbar_arrive(smem_u32(&sh.raw_empty[raw]));
+        }
+        if (++stage == T::kStages) stage = 0, phase ^= 1;
+        if (++raw == T::kRawStages) raw = 0, raw_phase ^= 1;
+      }
+    }
+  } else {
+    // ---------------------------------------------------------------------------------- softmax
+    
+    const int g = warp >> 2, row = threadIdx.x & 127;
+    const uint32_t lanes = tmem + ((uint32_t)(warp & 3) << 21);  // this warp's 32 lanes
+    const uint32_t s_addr = lanes + g * 128, o_addr = lanes + 256 + g * 128;
+    uint32_t s_phase = 0, o_phase = 0, odd = 0;
+    for (long long cur = begin, next = begin; cur < end; cur = next) {
+      int unit0, n, steps, hi, lo, hi_in, lo_in;
+      bool live;  // a row of the item (the tile may have others, and its lanes then hold anything)
+      {
+        const AttnItem it = attn_item(p, sh.prefix, cur, end);
+        next = cur + it.units;
+        n = it.units, unit0 = it.unit0;
+        const int t0 = it.tile * p.tile_tokens + (cp.two ? g * cp.half_tokens : 0);
+        const int tokens = max(0, min(min(it.seq.n - t0, cp.half_tokens), p.tile_tokens));
+        live = row < tokens * p.group;
+        steps = cp.two ? (tokens > 0 ? n : 0) : (n + 1 - g) >> 1;
+        const int first = it.seq.base + t0, last = first + tokens - 1, pos = first + row / p.group;
+        hi = pos + 1, lo = p.window > 0 ? max(0, pos - p.window + 1) : 0;
+        // keys that all of the group's rows see: units inside need no mask
+        hi_in = first + 1, lo_in = p.window > 0 ? max(0, last - p.window + 1) : 0;
+      }
+      float m = kNegInf, l = 0.f;
+      for (int j = 0; j < steps; ++j) {
+        wait(sh.s_full[g], s_phase);
+        s_phase ^= 1;
+        tmem_fence_after();
+        const int key0 = (unit0 + (cp.two ? j : 2 * j + g)) * kUnit;
+        const bool masked = key0 + kUnit > hi_in || key0 < lo_in;
+        auto mask = [&](float* s, int k0) {
+          if (masked) {
+#pragma unroll
+            for (int e = 0; e < 32; ++e)
+              if (key0 + k0 + e >= hi || key0 + k0 + e < lo) s[e] = kNegInf;
+          }
+        };
+        // The row's maximum here, a new reference from it where `wanted` says so, and what has been
+        // summed so far adapted to that.
+        auto refer = [&](float lag) {
+          float top = kNegInf;
+#pragma unroll 1
+          for (int k = 0; k < kUnit; k += 32) {
+            uint32_t bits[32];
+            float* s = reinterpret_cast<float*>(bits);
+            tmem_ld32(bits, s_addr + k);
+            tmem_wait_ld();
+            mask(s, k);
+#pragma unroll
+            for (int e = 0; e < 32; ++e) top = fmaxf(top, s[e]);
+          }
+          top *= p.scale_log2;
+          if (!__any_sync(0xffffffffu, live && top > m + lag)) return;
+          const float next = fmaxf(m, top), f = next == kNegInf ? 1.f : ex2(m - next);
+          m = next;
+          l *= f;
+          if (j > 0) {
+#pragma unroll 1
+            for (int k = 0; k < D; k += 16) {
+              uint32_t o[16];
+              tmem_ld16(o, o_addr + k);
+              tmem_wait_ld();
+#pragma unroll
+              for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
+              tmem_st16(o_addr + k, o);
+            }
+          }
+        };
+        float2 sum[2];
+        float over[2];
+        auto weigh = [&](uint32_t* bits, int k0, uint32_t* w) {  // 32 scores to 16 pairs of weights
+          const float ref = m == kNegInf ? 0.f : m;
+          const float2 sc2 = make_float2(p.scale_log2, p.scale_log2), mr2 = make_float2(-ref, -ref);
+          float* s = reinterpret_cast<float*>(bits);
+          mask(s, k0);
+#pragma unroll
+          for (int k = 0; k < 16; ++k) {
+            float2 z = fma2(make_float2(s[2 * k], s[2 * k + 1]), sc2, mr2);
+            if (!T::kMaxFirst) over[k & 1] = fmaxf(fmaxf(over[k & 1], z.x), z.y);
+            z.x = ex2(z.x);
+            z.y = ex2(z.y);
+            sum[k & 1] = add2(sum[k & 1], z);
+            const __half2 hw = __floats2half2_rn(z.x, z.y);
+            w[k] = *reinterpret_cast<const uint32_t*>(&hw);
+          }
+        };
+        if (T::kMaxFirst) {
+          refer(kLag);
+          sum[0] = sum[1] = make_float2(0.f, 0.f);
+          // weights over the scores already taken: 16 columns behind 32
+#pragma unroll 1
+          for (int c = 0; c < 4; ++c) {
+            uint32_t bits[32], w[16];
+            tmem_ld32(bits, s_addr + 32 * c);
+            tmem_wait_ld();
+            weigh(bits, 32 * c, w);
+            tmem_st16(s_addr + 16 * c, w);
+          }
+        } else {
+          uint32_t w[kUnit / 2];
+          // a reference is wanted in the first unit that a row sees something of
+          if (__any_sync(0xffffffffu, live && m == kNegInf && key0 < hi && key0 + kUnit > lo)) refer(0.f);
+          for (;;) {
+            sum[0] = sum[1] = make_float2(0.f, 0.f);
+            over[0] = over[1] = kNegInf;
+            uint32_t bits[2][32];
+            tmem_ld32(bits[0], s_addr);
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+              tmem_wait_ld();
+              if (c < 3) tmem_ld32(bits[(c + 1) & 1], s_addr + 32 * (c + 1));
+              weigh(bits[c & 1], 32 * c, w + 16 * c);
+            }
+            if (!__any_sync(0xffffffffu, live && fmaxf(over[0], over[1]) > kTop)) break;
+            refer(0.f);
+          }
+          tmem_st32(s_addr, w);
+          tmem_st32(s_addr + 32, w + 32);
+        }
+        l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
+        tmem_wait_st();
+        tmem_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&sh.p_full[g]));
+      }
+      // ------------------------------------------------------------------------------- the results
+      if (steps > 0) {
+        wait(sh.o_full[g], o_phase);
+        o_phase ^= 1;
+      }
+      odd ^= 1;
+      if (!cp.two && g == 1) sh.m1[odd][row] = m, sh.l1[odd][row] = l;
+      named_barrier<1>(256);
+      tmem_fence_after();
+      const AttnItem it = attn_item(p, sh.prefix, cur, end);  // again: not kept over the loop above
+      const int t0 = it.tile * p.tile_tokens + (cp.two ? g * cp.half_tokens : 0);
+      const int c0 = split.cta_of(it.item_first), c1 = split.cta_of(it.item_first + it.item_units - 1);
+      // With one row tile the first group joins both accumulators (the lanes are the same).
+      const bool writer = cp.two ? true : g == 0;
+      float fa = 1.f, fb = 0.f;
+      if (!cp.two && g == 0) {
+        const float m1 = sh.m1[odd][row], l1 = sh.l1[odd][row], top = fmaxf(m, m1);
+        fa = top == kNegInf ? 0.f : ex2(m - top);
+        fb = top == kNegInf ? 0.f : ex2(m1 - top);
+        m = top;
+        l = l * fa + l1 * fb;
+      }
+      const bool both = !cp.two && n > 1;
+      const int tok = it.seq.q0 + t0 + row / p.group, head = it.head * p.group + row % p.group;
+      const bool mine = writer && live;
+      constexpr size_t kSlot = (size_t)2 * kRowsTile * (128 + 2);  // floats: [D/4][256][4], then m, l
+      float* slot = p.slots + (2 * (size_t)blockIdx.x + ((int)blockIdx.x == c0 ? 1 : 0)) * kSlot;
+      const int slot_row = g * kRowsTile + row;
+      auto store_row = [&](int d, const float* v) {  // 16 elements of this thread's row, as fp16
+        __half* o = p.out + (long long)tok * p.out_ld + (long long)head * D + d;
+        uint32_t w[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const __half2 h = __floats2half2_rn(v[2 * e], v[2 * e + 1]);
+          w[e] = *reinterpret_cast<const uint32_t*>(&h);
+        }
+        if ((reinterpret_cast<uintptr_t>(o) & 15) == 0) {
+          reinterpret_cast<uint4*>(o)[0] = make_uint4(w[0], w[1], w[2], w[3]);
+          reinterpret_cast<uint4*>(o)[1] = make_uint4(w[4], w[5], w[6], w[7]);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) reinterpret_cast<uint32_t*>(o)[e] = w[e];
+        }
+      };
+      auto store_lse = [&](float top, float total) {
+        if (p.lse)
+          p.lse[(long long)tok * p.q_heads + head] =
+              total > 0.f ? (top + log2f(total)) * 0.6931471805599453f : total == 0.f ? kNegInf : total;
+      };
+      if (writer && steps > 0) {
+        const float inv = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll 1
+        for (int d = 0; d < D; d += 16) {
+          uint32_t x[16], y[16];
+          float* v = reinterpret_cast<float*>(x);
+          tmem_ld16(x, o_addr + d);
+          if (both) tmem_ld16(y, o_addr + 128 + d);
+          tmem_wait_ld();
+          if (!cp.two) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+              v[e] *= fa;
+              if (both) v[e] = fmaf(__uint_as_float(y[e]), fb, v[e]);
+            }
+          }
+          if (c0 == c1) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) v[e] = l == 0.f ? 0.f : v[e] * inv;
+            if (mine) store_row(d, v);
+          } else {
+#pragma unroll
+            for (int e = 0; e < 16; e += 4)
+              __stcg(reinterpret_cast<float4*>(slot) + ((d + e) / 4) * 256 + slot_row,
+                     make_float4(v[e], v[e + 1], v[e + 2], v[e + 3]));
+          }
+        }
+      }
+      tmem_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(smem_u32(&sh.o_free));
+      if (c0 == c1) {
+        if (mine && steps > 0) store_lse(m, l);
+      } else {
+        if (writer) {
+          __stcg(slot + D * 256 + slot_row, m);
+          __stcg(slot + D * 256 + 256 + slot_row, l);
+        }
+        __threadfence();
+        named_barrier<1>(256);
+        if (threadIdx.x == 0) {
+          const unsigned before = atomicAdd(p.counters + c0, 1u);
+          sh.is_last = before == (unsigned)(c1 - c0);
+          if (sh.is_last) p.counters[c0] = 0;
+        }
+        named_barrier<1>(256);
+        if (sh.is_last && mine) {
+          __threadfence();
+          const int parts = c1 - c0 + 1;
+          auto part = [&](int i) { return p.slots + (2 * (size_t)(c0 + i) + (i == 0 ? 1 : 0)) * kSlot; };
+          float top = kNegInf, total = 0.f;
+#pragma unroll 4
+          for (int i = 0; i < parts; ++i) top = fmaxf(top, __ldcg(part(i) + D * 256 + slot_row));
+#pragma unroll 4
+          for (int i = 0; i < parts; ++i) {
+            const float f = top == kNegInf ? 0.f : ex2(__ldcg(part(i) + D * 256 + slot_row) - top);
+            total = fmaf(__ldcg(part(i) + D * 256 + 256 + slot_row), f, total);
+          }
+          const float inv = total == 0.f ? 0.f : 1.f / total;
+#pragma unroll 1
+          for (int d = 0; d < D; d += 16) {
+            float v[16];
+#pragma unroll
+            for (int e = 0; e < 16; ++e) v[e] = 0.f;
+#pragma unroll 2
+            for (int i = 0; i < parts; ++i) {
+              const float f = top == kNegInf ? 0.f : ex2(__ldcg(part(i) + D * 256 + slot_row) - top);
+#pragma unroll
+              for (int e = 0; e < 16; e += 4) {
+                const float4 x = __ldcg(reinterpret_cast<const float4*>(part(i)) + ((d + e) / 4) * 256 + slot_row);
+                v[e] = fmaf(x.x, f, v[e]), v[e + 1] = fmaf(x.y, f, v[e + 1]);
+                v[e + 2] = fmaf(x.z, f, v[e + 2]), v[e + 3] = fmaf(x.w, f, v[e + 3]);
+              }
+            }
+#pragma unroll
+            for (int e = 0; e < 16; ++e) v[e] = total == 0.f ? 0.f : v[e] * inv;
+            store_row(d, v);
+          }
+          store_lse(top, total);
+        }
+      }
+    }
+  }
+  tmem_fence_before();
+  __syncthreads();
+  tmem_fence_after();
+  if (warp == T::kMmaWarp) tmem_free(tmem, 512);
+}
+
+template <int FMT, int D>
+cudaError_t launch(const qtea_kv* kv, const ChunkParams& cp, const CUtensorMap& map_q, cudaStream_t st) {
+  using T = Chunk<FMT, D>;
+  static_assert(T::kSmem + sizeof(ChunkShared) <= 227 * 1024, "shared memory of a CTA");
+  auto k = qtea_attn_chunk_kernel<FMT, D>;
+  cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, T::kSmem);
+  if (e != cudaSuccess) return e;
+  k<<<std::min(kv->sm_count, kAttnCounters), T::kThreads, T::kSmem, st>>>(kv->map_k, kv->map_v, map_q, cp);
+  return cudaGetLastError();
+}
+
+template <int FMT>
+cudaError_t launch_dim(const qtea_kv* kv, const ChunkParams& cp, const CUtensorMap& map_q, cudaStream_t st) {
+  return kv->view.dim == 128 ? launch<FMT, 128>(kv, cp, map_q, st) : launch<FMT, 64>(kv, cp, map_q, st);
+}
+
+}  // namespace
+
+size_t attn_chunk_floats(int sm_count) {
+  return (size_t)std::min(sm_count, kAttnCounters) * 2 * kRowsTile * (128 + 2);
+}
+
+cudaError_t launch_attn_chunk(const qtea_kv* kv, const AttnParams& base, cudaStream_t st) {
+  ChunkParams cp;
+  std::memset(&cp, 0, sizeof(cp));
+  cp.a = base;
+  AttnParams& p = cp.a;
+  cp.half_tokens = kRowsTile / p.group;
+  cp.two = p.b.max_q > cp.half_tokens;
+  p.tile_tokens = cp.two ? 2 * cp.half_tokens : cp.half_tokens;
+  p.unit_shift = 7;
+  p.min_units = 2;
+  const bool negative = p.scale_log2 < 0.f;
+  cp.q_flip = negative ? 0x80008000u : 0u;
+  // a masked score is -infinity before it is scaled: a scale of zero becomes one that is zero in effect
+  p.scale_log2 = std::max(std::fabs(p.scale_log2), 1e-30f);
+  CUtensorMap map_q;
+  std::memset(&map_q, 0, sizeof(map_q));
+  if (!negative && reinterpret_cast<uintptr_t>(p.q) % 16 == 0 && p.q_ld % 8 == 0 && p.q_ld * 2 < (1ll << 40)) {
+    const int dim = kv->view.dim;
+    cuuint64_t dims[3] = {(cuuint64_t)dim, (cuuint64_t)p.q_heads, (cuuint64_t)p.b.n_tokens};
+    cuuint64_t strides[2] = {(cuuint64_t)dim * 2, (cuuint64_t)p.q_ld * 2};
+    cuuint32_t box[3] = {64, (cuuint32_t)p.group, (cuuint32_t)cp.half_tokens};
+    cuuint32_t step[3] = {1, 1, 1};
+    cp.q_map = reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(kv->encode)(
+                   &map_q, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, const_cast<__half*>(p.q), dims, strides, box, step,
+                   CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+  }
+  if (kv->view.format == QTEA_KV_F16) return launch_dim<QTEA_KV_F16>(kv, cp, map_q, st);
+  if (kv->view.format == QTEA_KV_FP8) return launch_dim<QTEA_KV_FP8>(kv, cp, map_q, st);
+  return launch_dim<QTEA_KV_FP4>(kv, cp, map_q, st);
+}
+
+}  // namespace qtea

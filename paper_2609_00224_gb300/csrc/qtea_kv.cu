@@ -334,6 +334,7 @@ int qtea_kv_create(void* k_pages, void* v_pages, void* k_scales, void* v_scales,
                     static_cast<uint8_t*>(v_scales), n_pages, page_size, n_kv_heads, head_dim, format, shift};
   kv->device = dev;
   kv->sm_count = sms;
+  kv->encode = fn;
   // Rows of codes as a matrix of bytes; a box is 16 tokens by at most 128 bytes, so that pages of
   // any size are whole boxes and the swizzle spans a box's row: reading 8 rows at one place of the
   // row, as the fragment loads do, then touches every bank once.

@@ -122,6 +122,6 @@ __device__ __forceinline__ uint32_t scale_bits(uint32_t byte) { return ((byte - 
 struct qtea_kv {
   qtea::KvView view;
   int device, sm_count;
-  // Tensor maps of the codes, rows of 64 or 128 bytes ... (see qtea_attn.cu, qtea_attn_chunk.cu)
-  CUtensorMap map_k, map_v;
+  void* encode;              // the driver's cuTensorMapEncodeTiled
+  CUtensorMap map_k, map_v;  // the codes in boxes of 16 tokens by at most 128 bytes, swizzled
 };

@@ -141,6 +141,14 @@ ATT = [
     ("a prompt", [150], [150], 8, 2, 128, 16, 0),
     ("a chunk after others", [70, 1, 130], [300, 9, 131], 8, 2, 64, 32, 0),
     ("a windowed prompt", [140], [200], 8, 4, 128, 16, 37),
+    ("a prompt, group of 5", [60], [60], 10, 2, 128, 16, 0),
+    ("16 tokens, group of 8", [16, 16, 16], [300, 16, 129], 16, 2, 128, 64, 0),
+    ("prompt and decode steps", [200, 1, 1, 33], [200, 700, 3, 40], 8, 2, 128, 32, 0),
+    ("small chunk over many units", [40, 3], [3000, 2000], 4, 1, 128, 64, 0),
+    ("two row tiles over many units", [70], [1800], 4, 1, 64, 128, 0),
+    ("windows through row tiles", [130, 90], [500, 90], 4, 1, 64, 16, 64),
+    ("nine tokens, group of 32", [9], [100], 32, 1, 64, 16, 0),
+    ("a chunk with empty rows", [50, 40], [20, 0], 4, 2, 64, 16, 0),
     ("many sequences", [1] * 70, list(range(1, 71)), 4, 1, 64, 16, 0),
 ]
 
@@ -162,6 +170,33 @@ def test_attention_large_logits_and_negative_scale(qt):
     check_attention(c, q_scale=8.0)
     check_attention(c, scale=-0.2)
     check_attention(c, scale=0.0)
+
+
+@pytest.mark.parametrize("fmt", list(FMTS))
+@pytest.mark.parametrize("dim", [64, 128])
+def test_chunk_attention_large_logits_scales_and_alignment(qt, fmt, dim):
+    c = Case(qt, fmt, [100, 33], [400, 50], 4, 1, dim, 16, seed=31)
+    check_attention(c, q_scale=8.0)  # rows whose maximum grows by far more than fp16's range from unit to unit
+    check_attention(c, scale=-0.2)
+    check_attention(c, scale=0.0)
+    q = torch.randn(c.tokens, 4, dim, device="cuda").half()
+    ref = qt.qtea_attention(c.cache, c.batch, q)
+    flat = torch.zeros(c.tokens * (4 * dim + 2) + 2, device="cuda").half()
+    odd = flat[2:].view(c.tokens, 4 * dim + 2)[:, :4 * dim].unflatten(1, (4, dim))  # 4-byte aligned rows
+    odd.copy_(q)
+    out = torch.zeros_like(flat)[2:].view(c.tokens, 4 * dim + 2)[:, :4 * dim].unflatten(1, (4, dim))
+    qt.qtea_attention(c.cache, c.batch, odd, out=out)
+    assert torch.equal(out, ref)
+
+
+def test_chunk_attention_last_keys_dominate(qt):
+    """Keys that grow with their position: every unit outruns the reference of the one before."""
+    c = Case(qt, "f16", [40], [700], 4, 1, 128, 16, seed=32)
+    for p in range(700):
+        row = (c.seq["k"][0][p] * (1 + p / 40)).astype(np.float16)
+        c.seq["k"][0][p] = row.astype(np.float64)
+        c.t["k"][c.pages[0][p // 16], :, p % 16] = gpu(row)
+    check_attention(c)
 
 
 def test_attention_into_its_queries_and_strided_rows(qt):
