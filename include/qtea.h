@@ -471,7 +471,7 @@ void qtea_kv_free(qtea_kv* kv);
  * Lengths are read on the device, so a captured graph can be replayed with others. They are
  * bounded there: a context longer than max_pages * page_size counts as that long, a negative one
  * as empty, and page numbers outside [0, n_pages) are never followed out of the cache.
- * Limits: 1 <= n_seqs <= 1024 (n_seqs = 0: nothing to do), n_tokens >= 0, max_q_len >= 1, max_pages >= 1,
+ * Limits: 1 <= n_seqs <= 512 (n_seqs = 0: nothing to do), n_tokens >= 0, max_q_len >= 1, max_pages >= 1,
  * max_pages * page_size < 2^31.
  */
 typedef struct qtea_kv_batch {

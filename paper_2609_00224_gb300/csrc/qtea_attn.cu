@@ -31,7 +31,6 @@ namespace {
 constexpr int kWarps = 4;
 constexpr int kMaxRows = 32;
 constexpr float kLag = 8.f;
-constexpr int kRowsGrid = 320;  // the weights of that many parts fit the rings
 constexpr float kNegInf = -INFINITY;
 
 __device__ __forceinline__ float ex2(float x) {
@@ -63,6 +62,14 @@ __device__ __forceinline__ void mma16816(float* c, const uint32_t* a, uint32_t b
       : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
       : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
+// c = a * b
+__device__ __forceinline__ void mma16816_first(float* c, const uint32_t* a, uint32_t b0, uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
+      "{%10, %10, %10, %10};"
+      : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
+}
 __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
   asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst),
                "l"(reinterpret_cast<uint64_t>(src)), "r"(bytes), "r"(bar)
@@ -79,26 +86,39 @@ __device__ __forceinline__ uint32_t lds16(uint32_t a) {
   return r;
 }
 
-// Powers of two of block `blk` of two rows' scale words, as a pair of fp16 (see scale_bits).
-__device__ __forceinline__ uint32_t scale_pair(uint32_t w0, uint32_t w1, int blk) {
-  const uint32_t t = __byte_perm(w0, w1, blk | (4 + blk) << 8);  // in bytes 0 and 2, others beside them
-  return ((t & 0x001f001fu) ^ 0x00100010u) << 10;
+// A row's scale bytes as the high bytes of the fp16 powers of two that they stand for (113..142, the
+// exponents -14..15; their top bits are clear).
+__device__ __forceinline__ uint32_t scale_high(uint32_t w) { return ((w & 0x1f1f1f1fu) ^ 0x10101010u) << 2; }
+
+// Block `blk` of two such words as a pair of fp16; a selector with its own top bit set gives a byte of copies
+// of the selected byte's top bit: zeros.
+__device__ __forceinline__ uint32_t scale_pair(uint32_t h0, uint32_t h1, int blk) {
+  uint32_t r;
+  asm("prmt.b32 %0, %1, %2, %3;" : "=r"(r) : "r"(h0), "r"(h1), "r"((8 | blk) | blk << 4 | (12 | blk) << 8 | (4 | blk) << 12));
+  return r;
+}
+
+// The power of two of block `blk` of a row's scale word, as fp32: the byte is its exponent.
+__device__ __forceinline__ float scale_of(uint32_t w, int blk) {
+  return __uint_as_float((blk == 3 ? w >> 1 : w << (23 - 8 * blk)) & 0x7f800000u);
 }
 
 template <int FMT, int D, int NT>
 struct Rows {
-  static constexpr int kKeys = FMT == QTEA_KV_F16 ? 16 : FMT == QTEA_KV_FP8 ? 32 : 64;  // of a unit
-  static constexpr int kShift = FMT == QTEA_KV_F16 ? 4 : FMT == QTEA_KV_FP8 ? 5 : 6;
+  static constexpr int kKeys = 1 << kv_unit_shift(FMT);  // of a unit
+  static constexpr int kShift = kv_unit_shift(FMT);
   static constexpr int kRowBytes = FMT == QTEA_KV_F16 ? 2 * D : FMT == QTEA_KV_FP8 ? D : D / 2;
   static constexpr int kWide = kRowBytes < 128 ? kRowBytes : 128;  // bytes of a box's row
   static constexpr int kParts = kRowBytes / kWide;
-  static constexpr int kBoxes = kKeys / 16;
+  static constexpr int kSubs = kKeys / 16;  // a product takes 16 keys
   static constexpr int kBoxBytes = 16 * kWide;
   static constexpr int kSideBytes = kKeys * kRowBytes;
   static constexpr int kScaleRow = D / kKvBlock;
   static constexpr int kScaleBytes = FMT == QTEA_KV_F16 ? 0 : kKeys * kScaleRow;
   static constexpr int kStageBytes = 2 * kSideBytes;
-  static constexpr int kStages = NT == 4 && D == 128 ? 2 : 3;  // two CTAs' rings fit an SM
+  // CTAs of an SM, as registers and rings allow: three of one column tile, two of more
+  static constexpr int kCtas = NT == 1 ? 3 : 2;
+  static constexpr int kStages = NT == 2 || D == 64 ? 3 : 2;
   static constexpr int kMaskXor = kWide == 128 ? 7 : kWide == 64 ? 3 : 1;
   static constexpr int kRing = kWarps * kStages * kStageBytes;
   static constexpr int kScaleRing = kWarps * kStages * 2 * kScaleBytes;
@@ -113,16 +133,16 @@ __device__ __forceinline__ uint32_t swizzled(int r, int x) {
 
 // NT column tiles of 8 query rows.
 template <int FMT, int D, int NT>
-__global__ void __launch_bounds__(kWarps * 32, 2)
+__global__ void __launch_bounds__(kWarps * 32, (Rows<FMT, D, NT>::kCtas))
     qtea_attn_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
                           const AttnParams p) {
   using T = Rows<FMT, D, NT>;
   constexpr int R = 8 * NT, KS = D / 16, MT = D / 16;
   extern __shared__ __align__(1024) uint8_t smem[];  // the rings, then reused to join results
-  __shared__ long long prefix[kKvMaxSeqs + 1];
   __shared__ __align__(8) uint64_t full[kWarps][T::kStages];
   __shared__ float stat_m[kWarps][R], stat_l[kWarps][R], joined_m[R], joined_l[R];
   __shared__ int is_last;
+  __shared__ int span[3], end;
   // Q^T fragments of four column tiles do not fit the registers beside O^T: they are read from here
   constexpr bool kQShared = NT == 4;
   __shared__ uint2 q_shared[kQShared ? KS * NT * 32 : 1];
@@ -133,48 +153,72 @@ __global__ void __launch_bounds__(kWarps * 32, 2)
     for (int i = 0; i < T::kStages; ++i) mbar_init(smem_u32(&full[warp][i]), 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  attn_prefix(p, prefix);
-  const AttnSplit split = attn_split(p, prefix);
-  if (split.total == 0 || (int)blockIdx.x >= split.ctas) return;
-  const long long end = split.first(blockIdx.x + 1);
+  const AttnTable tab = attn_table(smem + T::kRing + T::kScaleRing, p.b.n_seqs);
+  attn_prefix(p, tab);
+  int cur;
+  {
+    const AttnSplit split = attn_split(p, tab);
+    if (split.total == 0 || (int)blockIdx.x >= split.ctas) return;
+    cur = split.first(blockIdx.x);
+    if (threadIdx.x == 0) end = split.first(blockIdx.x + 1);
+    __syncthreads();
+  }
 
+  // Byte offsets within a box of this lane's fragment rows, one per 32 bytes of a row: keys as rows
+  // (K), keys as columns (V, transposed on the way).
+  constexpr int kOffsets = T::kWide / 32 > 0 ? T::kWide / 32 : 1;
+  uint32_t k_off[kOffsets], v_off[kOffsets];
+#pragma unroll
+  for (int i = 0; i < kOffsets; ++i) {
+    k_off[i] = swizzled<T>((lane & 7) + (lane >> 3 & 1) * 8, 32 * i + (lane >> 4) * 16);
+    v_off[i] = swizzled<T>((lane & 7) + (lane >> 4) * 8, 32 * i + (lane >> 3 & 1) * 16);
+  }
   const uint32_t ring = smem_u32(smem) + warp * T::kStages * T::kStageBytes;
   const uint32_t scales = smem_u32(smem) + T::kRing + warp * T::kStages * 2 * T::kScaleBytes;
   float* join = reinterpret_cast<float*>(smem);
+  const int box = min(p.kv.page_size, T::kKeys), boxes = T::kKeys / box;  // tokens of a copy, copies of a unit
   uint32_t fills = 0;  // stages this warp has consumed, over all items
   bool ok = true;
 
-  for (long long cur = split.first(blockIdx.x); cur < end;) {
-    const AttnItem it = attn_item(p, prefix, cur, end);
-    cur += it.units;
+  while (cur < end) {
+    const AttnItem it = attn_item(p, tab, cur, end);
+    if (it.units == 0) {
+      cur = it.next;
+      continue;
+    }
+    if (threadIdx.x == 0) {  // not kept in registers over the loop below
+      span[0] = it.first;
+      span[1] = it.last;
+      span[2] = it.next;
+    }
     const int mine = (it.units - warp + kWarps - 1) / kWarps;  // units unit0 + warp + kWarps * i
     const int* pages = p.b.pages + (long long)it.s * p.b.max_pages;
 
-    // The copies of this warp's unit i: a box of 16 tokens per lane. Its page number was loaded
-    // when the box before it was issued.
+    // The copies of this warp's unit i, a box per lane. Its page number was loaded when the box before
+    // it was issued.
     auto page_of = [&](int i) {
-      const int key = ((it.unit0 + warp + kWarps * i) << T::kShift) + 16 * lane;
+      const int key = ((it.unit0 + warp + kWarps * i) << T::kShift) + box * lane;
       return __ldg(pages + min(key >> p.kv.page_shift, p.b.max_pages - 1));
     };
-    int next_page = lane < T::kBoxes && mine > 0 ? page_of(0) : 0;
+    int next_page = lane < boxes && mine > 0 ? page_of(0) : 0;
     auto issue = [&](int i, uint32_t stage) {
       const uint32_t bar = smem_u32(&full[warp][stage]);
       if (lane == 0) mbar_arrive_expect_tx(bar, T::kStageBytes + 2 * T::kScaleBytes);
       __syncwarp();
-      if (lane < T::kBoxes) {
-        const int key = ((it.unit0 + warp + kWarps * i) << T::kShift) + 16 * lane;
+      if (lane < boxes) {
+        const int key = ((it.unit0 + warp + kWarps * i) << T::kShift) + box * lane;
         const int page = min(max(next_page, 0), p.kv.n_pages - 1);
         const int row = (page * p.kv.heads + it.head) * p.kv.page_size + (key & (p.kv.page_size - 1));
-        const uint32_t dst = ring + stage * T::kStageBytes + lane * T::kParts * T::kBoxBytes;
+        const uint32_t dst = ring + stage * T::kStageBytes + lane * box * T::kWide;
 #pragma unroll
         for (int h = 0; h < T::kParts; ++h) tma_load_2d(dst + h * T::kBoxBytes, &map_k, h * T::kWide, row, bar);
 #pragma unroll
         for (int h = 0; h < T::kParts; ++h)
           tma_load_2d(dst + T::kSideBytes + h * T::kBoxBytes, &map_v, h * T::kWide, row, bar);
         if (FMT != QTEA_KV_F16) {
-          const uint32_t sd = scales + stage * 2 * T::kScaleBytes + lane * 16 * T::kScaleRow;
-          bulk_load(sd, p.kv.ks + (long long)row * T::kScaleRow, 16 * T::kScaleRow, bar);
-          bulk_load(sd + T::kScaleBytes, p.kv.vs + (long long)row * T::kScaleRow, 16 * T::kScaleRow, bar);
+          const uint32_t sd = scales + stage * 2 * T::kScaleBytes + lane * box * T::kScaleRow;
+          bulk_load(sd, p.kv.ks + (long long)row * T::kScaleRow, box * T::kScaleRow, bar);
+          bulk_load(sd + T::kScaleBytes, p.kv.vs + (long long)row * T::kScaleRow, box * T::kScaleRow, bar);
         }
         if (i + 1 < mine) next_page = page_of(i + 1);
       }
@@ -185,30 +229,19 @@ __global__ void __launch_bounds__(kWarps * 32, 2)
       st_issue = st_issue + 1 == T::kStages ? 0 : st_issue + 1;
     }
 
-    // This thread's query rows: 8 nt + 2c and the next (columns of S^T and O^T), and the keys that
-    // each sees, [lo, hi).
     const int i0 = it.tile * p.tile_tokens, rows = min(it.seq.n - i0, p.tile_tokens) * p.group;
-    int lo[NT][2], hi[NT][2];
-    int lo_all = 0x7fffffff, hi_all = 0, lo_in = 0, hi_in = 0x7fffffff;
-    for (int r = 0; r < rows; r += p.group) {  // once per token: uniform bounds over the tile
-      const int pos = it.seq.base + i0 + r / p.group;
-      const int l = p.window > 0 ? max(0, pos - p.window + 1) : 0, h = pos + 1;
-      lo_all = min(lo_all, l), hi_all = max(hi_all, h), lo_in = max(lo_in, l), hi_in = min(hi_in, h);
-    }
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const int r = 8 * nt + 2 * c + e, pos = it.seq.base + i0 + r / p.group;
-        hi[nt][e] = r < rows ? pos + 1 : 0;
-        lo[nt][e] = p.window > 0 ? max(0, pos - p.window + 1) : 0;
-      }
+    // keys that some token of the tile sees, and keys that all do
+    const int first = it.seq.base + i0, last = it.seq.base + min(it.seq.n, i0 + p.tile_tokens) - 1;
+    const int lo_all = p.window > 0 ? max(0, first - p.window + 1) : 0, hi_all = max(last + 1, 0);
+    const int lo_in = p.window > 0 ? max(0, last - p.window + 1) : 0, hi_in = first + 1;
+    // The keys that query row r sees: up to here and, with a window, from this less the window.
+    auto seen = [&](int r) { return r < rows ? it.seq.base + i0 + attn_token(p, r) + 1 : 0; };
 
     // Q^T fragments: column (query row) 8 nt + g, head_dim in the order of the format's codes.
     uint2 qf[kQShared ? 1 : KS][NT];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
-      const int r = 8 * nt + g, tok = it.seq.q0 + i0 + r / p.group, h = it.head * p.group + r % p.group;
+      const int r = 8 * nt + g, tok = it.seq.q0 + i0 + attn_token(p, r), h = it.head * p.group + r - attn_token(p, r) * p.group;
       const __half* row = p.q + (long long)tok * p.q_ld + (long long)h * D;
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) {
@@ -227,13 +260,15 @@ __global__ void __launch_bounds__(kWarps * 32, 2)
       }
     }
     if (kQShared) __syncthreads();
-    auto mma_q = [&](float* acc, const uint32_t* a, int ks, int nt) {
+    auto mma_q = [&](float* acc, const uint32_t* a, int ks, int nt, bool first) {
       const uint2 b = kQShared ? q_shared[(ks * NT + nt) * 32 + lane] : qf[kQShared ? 0 : ks][nt];
-      mma16816(acc, a, b.x, b.y);
+      if (first) mma16816_first(acc, a, b.x, b.y);
+      else mma16816(acc, a, b.x, b.y);
     };
 
     float o[MT][NT][4];
-    float m[NT][2], l[NT][2];  // the reference (-infinity while nothing has been seen) and this thread's sums
+    // the reference (-infinity while nothing has been seen), and this thread's sums
+    float m[NT][2], l[NT][2];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) m[nt][0] = m[nt][1] = kNegInf, l[nt][0] = l[nt][1] = 0.f;
 #pragma unroll
@@ -250,78 +285,92 @@ __global__ void __launch_bounds__(kWarps * 32, 2)
       const uint32_t kbase = ring + stage * T::kStageBytes, vbase = kbase + T::kSideBytes;
       const uint32_t sbase = scales + stage * 2 * T::kScaleBytes;
       const int key_unit = (it.unit0 + warp + kWarps * i) << T::kShift;
-#pragma unroll 1
-      for (int sub = 0; sub < T::kBoxes; ++sub) {
+#pragma unroll (FMT == QTEA_KV_F16 || NT == 4 ? 1 : 2)
+      for (int sub = 0; sub < T::kSubs; ++sub) {
         const int key0 = key_unit + 16 * sub;
         if (key0 >= hi_all || key0 + 16 <= lo_all) continue;  // nothing of the tile sees these
         const uint32_t kb = kbase + sub * T::kParts * T::kBoxBytes, vb = vbase + sub * T::kParts * T::kBoxBytes;
         float s[NT][4];
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) s[nt][0] = s[nt][1] = s[nt][2] = s[nt][3] = 0.f;
         {
-          const int kr = (lane & 7) + (lane >> 3 & 1) * 8, kx = (lane >> 4) * 16;
           if (FMT == QTEA_KV_F16) {
+            float odd[NT][4];  // every second product: half the chain
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks) {
               const int x = 32 * ks;
               uint32_t a[4];
-              ldmatrix4(a, kb + (x / T::kWide) * T::kBoxBytes + swizzled<T>(kr, x % T::kWide + kx));
+              ldmatrix4(a, kb + k_off[x % T::kWide / 32] + (x / T::kWide) * T::kBoxBytes);
 #pragma unroll
-              for (int nt = 0; nt < NT; ++nt) mma_q(s[nt], a, ks, nt);
+              for (int nt = 0; nt < NT; ++nt) mma_q(ks & 1 ? odd[nt] : s[nt], a, ks, nt, ks < 2);
             }
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) s[nt][e] += odd[nt][e];
           } else {
+            // a block's codes are multiplied as they are, and its sum by the rows' powers of two
             const uint32_t sk = sbase + sub * 16 * T::kScaleRow;
             const uint32_t w0 = D == 128 ? lds32(sk + g * 4) : lds16(sk + g * 2);
             const uint32_t w1 = D == 128 ? lds32(sk + (g + 8) * 4) : lds16(sk + (g + 8) * 2);
+            auto add_block = [&](int blk, const uint32_t* a0, const uint32_t* a1) {
+              const float f0 = scale_of(w0, blk), f1 = scale_of(w1, blk);
+#pragma unroll
+              for (int nt = 0; nt < NT; ++nt) {
+                float t[4];
+                mma_q(t, a0, 2 * blk, nt, true);
+                mma_q(t, a1, 2 * blk + 1, nt, false);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                  const float f = e < 2 ? f0 : f1;
+                  s[nt][e] = blk == 0 ? t[e] * f : fmaf(t[e], f, s[nt][e]);
+                }
+              }
+            };
 #pragma unroll
             for (int x = 0; x < T::kRowBytes; x += 32) {
               uint32_t r[4];
-              ldmatrix4(r, kb + swizzled<T>(kr, x + kx));
+              ldmatrix4(r, kb + k_off[x / 32]);
               if (FMT == QTEA_KV_FP8) {
-                const int blk = x / 32;
-                const uint32_t f0 = scale_pair(w0, w0, blk), f1 = scale_pair(w1, w1, blk);
-#pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                  const uint32_t a[4] = {hmul2(from_e4m3x2(r[2 * j]), f0), hmul2(from_e4m3x2(r[2 * j + 1]), f1),
-                                         hmul2(from_e4m3x2_hi(r[2 * j]), f0), hmul2(from_e4m3x2_hi(r[2 * j + 1]), f1)};
-#pragma unroll
-                  for (int nt = 0; nt < NT; ++nt) mma_q(s[nt], a, 2 * blk + j, nt);
-                }
+                const uint32_t a0[4] = {from_e4m3x2(r[0]), from_e4m3x2(r[1]), from_e4m3x2_hi(r[0]), from_e4m3x2_hi(r[1])};
+                const uint32_t a1[4] = {from_e4m3x2(r[2]), from_e4m3x2(r[3]), from_e4m3x2_hi(r[2]), from_e4m3x2_hi(r[3])};
+                add_block(x / 32, a0, a1);
               } else {
 #pragma unroll
                 for (int hb = 0; hb < 2; ++hb) {
-                  const int blk = x / 16 + hb;
-                  if (blk >= D / 32) break;
-                  const uint32_t f0 = scale_pair(w0, w0, blk), f1 = scale_pair(w1, w1, blk);
+                  if (x / 16 + hb >= D / 32) break;
                   uint32_t e0[4], e1[4];
                   from_e2m1x8(r[2 * hb], e0);
                   from_e2m1x8(r[2 * hb + 1], e1);
-#pragma unroll
-                  for (int j = 0; j < 2; ++j) {
-                    const uint32_t a[4] = {hmul2(e0[2 * j], f0), hmul2(e1[2 * j], f1), hmul2(e0[2 * j + 1], f0),
-                                           hmul2(e1[2 * j + 1], f1)};
-#pragma unroll
-                    for (int nt = 0; nt < NT; ++nt) mma_q(s[nt], a, 2 * blk + j, nt);
-                  }
+                  const uint32_t a0[4] = {e0[0], e1[0], e0[1], e1[1]}, a1[4] = {e0[2], e1[2], e0[3], e1[3]};
+                  add_block(x / 16 + hb, a0, a1);
                 }
               }
             }
           }
         }
         // softmax weights
-        const bool masked = key0 + 16 > hi_in || key0 < lo_in;
         bool outrun = false;
+        if (key0 + 16 > hi_in || key0 < lo_in) {
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
+          for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            s[nt][e] *= p.scale_log2;
-            if (masked) {
-              const int key = key0 + g + (e >> 1) * 8;
-              if (key < lo[nt][e & 1] || key >= hi[nt][e & 1]) s[nt][e] = kNegInf;
+            for (int col = 0; col < 2; ++col) {
+              const int h = seen(8 * nt + 2 * c + col), l = p.window > 0 ? h - p.window : 0;
+#pragma unroll
+              for (int e = col; e < 4; e += 2) {
+                const int key = key0 + g + (e >> 1) * 8;
+                s[nt][e] = key < l || key >= h ? kNegInf : s[nt][e] * p.scale_log2;
+                outrun |= s[nt][e] > m[nt][col] + kLag;
+              }
             }
-            outrun |= s[nt][e] > m[nt][e & 1] + kLag;
-          }
+        } else {
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              s[nt][e] *= p.scale_log2;
+              outrun |= s[nt][e] > m[nt][e & 1] + kLag;
+            }
+        }
         if (__any_sync(0xffffffffu, outrun)) {
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt)
@@ -355,67 +404,68 @@ __global__ void __launch_bounds__(kWarps * 32, 2)
             pf[nt][h] = transpose8(*reinterpret_cast<const uint32_t*>(&w));
           }
         }
-        // O^T += V^T P^T. Where some keys lie outside all that the tile sees, their values are
-        // replaced by zeros: 0 * NaN would reach the sums.
-        uint32_t keep0 = 0xffffffffu, keep1 = 0xffffffffu;  // of keys 2c, 2c+1 and 2c+8, 2c+9
-        if (key0 + 16 > hi_all || key0 < lo_all) {
-          auto in = [&](int k) { return key0 + k >= lo_all && key0 + k < hi_all; };
-          keep0 = (in(2 * c) ? 0xffffu : 0u) | (in(2 * c + 1) ? 0xffff0000u : 0u);
-          keep1 = (in(2 * c + 8) ? 0xffffu : 0u) | (in(2 * c + 9) ? 0xffff0000u : 0u);
-        }
-        {
-          const int vr = (lane & 7) + (lane >> 4) * 8, vx = (lane >> 3 & 1) * 16;
-          if (FMT == QTEA_KV_F16) {
+        // O^T += V^T P^T. Where some keys lie outside all that the tile sees, their values and powers
+        // of two are replaced by zeros: 0 * NaN would reach the sums.
+        const bool edge = key0 + 16 > hi_all || key0 < lo_all;
+        auto in = [&](int k) { return key0 + k >= lo_all && key0 + k < hi_all; };
+        auto load_v = [&](uint32_t* r, uint32_t addr) {  // keys 2c, 2c+1 in r[0], r[1], 2c+8, 2c+9 in r[2], r[3]
+          ldmatrix4_trans(r, addr);
+          if (edge) {
+            const uint32_t k0 = (in(2 * c) ? 0xffffu : 0u) | (in(2 * c + 1) ? 0xffff0000u : 0u);
+            const uint32_t k1 = (in(2 * c + 8) ? 0xffffu : 0u) | (in(2 * c + 9) ? 0xffff0000u : 0u);
+            r[0] &= k0, r[1] &= k0, r[2] &= k1, r[3] &= k1;
+          }
+        };
+        if (FMT == QTEA_KV_F16) {
 #pragma unroll
-            for (int mt = 0; mt < MT; ++mt) {
-              const int x = 32 * mt;
-              uint32_t a[4];
-              ldmatrix4_trans(a, vb + (x / T::kWide) * T::kBoxBytes + swizzled<T>(vr, x % T::kWide + vx));
-              a[0] &= keep0, a[1] &= keep0, a[2] &= keep1, a[3] &= keep1;
+          for (int mt = 0; mt < MT; ++mt) {
+            const int x = 32 * mt;
+            uint32_t a[4];
+            load_v(a, vb + v_off[x % T::kWide / 32] + (x / T::kWide) * T::kBoxBytes);
 #pragma unroll
-              for (int nt = 0; nt < NT; ++nt) mma16816(o[mt][nt], a, pf[nt][0], pf[nt][1]);
-            }
-          } else {
-            const uint32_t sv = sbase + T::kScaleBytes + sub * 16 * T::kScaleRow;
-            uint32_t w[4];
+            for (int nt = 0; nt < NT; ++nt) mma16816(o[mt][nt], a, pf[nt][0], pf[nt][1]);
+          }
+        } else {
+          const uint32_t sv = sbase + T::kScaleBytes + sub * 16 * T::kScaleRow;
+          uint32_t w[4];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              const int key = 2 * c + (j & 1) + (j >> 1) * 8;
-              w[j] = D == 128 ? lds32(sv + key * 4) : lds16(sv + key * 2);
-            }
+          for (int j = 0; j < 4; ++j) {
+            const int key = 2 * c + (j & 1) + (j >> 1) * 8;
+            w[j] = D == 128 ? lds32(sv + key * 4) : lds16(sv + key * 2);
+            w[j] = scale_high(edge && !in(key) ? 0x7f7f7f7fu : w[j]);
+          }
 #pragma unroll
-            for (int x = 0; x < T::kRowBytes; x += 32) {
-              uint32_t r[4];
-              ldmatrix4_trans(r, vb + swizzled<T>(vr, x + vx));
-              if (FMT == QTEA_KV_FP8) {
-                const int blk = x / 32;
+          for (int x = 0; x < T::kRowBytes; x += 32) {
+            uint32_t r[4];
+            load_v(r, vb + v_off[x / 32]);
+            if (FMT == QTEA_KV_FP8) {
+              const int blk = x / 32;
+              const uint32_t f0 = scale_pair(w[0], w[1], blk), f1 = scale_pair(w[2], w[3], blk);
+#pragma unroll
+              for (int j = 0; j < 2; ++j) {  // codes 16 j + 2g and the next
+                const uint32_t t0 = __byte_perm(r[j], 0, 0x3120), t1 = __byte_perm(r[2 + j], 0, 0x3120);
+                const uint32_t a[4] = {hmul2(from_e4m3x2(t0), f0), hmul2(from_e4m3x2_hi(t0), f0),
+                                       hmul2(from_e4m3x2(t1), f1), hmul2(from_e4m3x2_hi(t1), f1)};
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) mma16816(o[2 * blk + j][nt], a, pf[nt][0], pf[nt][1]);
+              }
+            } else {
+#pragma unroll
+              for (int hb = 0; hb < 2; ++hb) {
+                const int blk = x / 16 + hb;
+                if (blk >= D / 32) break;
                 const uint32_t f0 = scale_pair(w[0], w[1], blk), f1 = scale_pair(w[2], w[3], blk);
+                uint32_t e0[4], e1[4];
+                from_e2m1x8(r[hb], e0);
+                from_e2m1x8(r[2 + hb], e1);
 #pragma unroll
-                for (int j = 0; j < 2; ++j) {  // codes 16 j + 2g and the next
-                  const uint32_t t0 = __byte_perm(r[j], 0, 0x3120), t1 = __byte_perm(r[2 + j], 0, 0x3120);
-                  const uint32_t a[4] = {hmul2(from_e4m3x2(t0), f0) & keep0, hmul2(from_e4m3x2_hi(t0), f0) & keep0,
-                                         hmul2(from_e4m3x2(t1), f1) & keep1, hmul2(from_e4m3x2_hi(t1), f1) & keep1};
+                for (int j = 0; j < 2; ++j) {  // codes 4g + 2j and the next
+                  const uint32_t a[4] = {hmul2(__byte_perm(e0[j], e0[2 + j], 0x5410), f0),
+                                         hmul2(__byte_perm(e0[j], e0[2 + j], 0x7632), f0),
+                                         hmul2(__byte_perm(e1[j], e1[2 + j], 0x5410), f1),
+                                         hmul2(__byte_perm(e1[j], e1[2 + j], 0x7632), f1)};
 #pragma unroll
                   for (int nt = 0; nt < NT; ++nt) mma16816(o[2 * blk + j][nt], a, pf[nt][0], pf[nt][1]);
-                }
-              } else {
-#pragma unroll
-                for (int hb = 0; hb < 2; ++hb) {
-                  const int blk = x / 16 + hb;
-                  if (blk >= D / 32) break;
-                  const uint32_t f0 = scale_pair(w[0], w[1], blk), f1 = scale_pair(w[2], w[3], blk);
-                  uint32_t e0[4], e1[4];
-                  from_e2m1x8(r[hb], e0);
-                  from_e2m1x8(r[2 + hb], e1);
-#pragma unroll
-                  for (int j = 0; j < 2; ++j) {  // codes 4g + 2j and the next
-                    const uint32_t a[4] = {hmul2(__byte_perm(e0[j], e0[2 + j], 0x5410), f0) & keep0,
-                                           hmul2(__byte_perm(e0[j], e0[2 + j], 0x7632), f0) & keep0,
-                                           hmul2(__byte_perm(e1[j], e1[2 + j], 0x5410), f1) & keep1,
-                                           hmul2(__byte_perm(e1[j], e1[2 + j], 0x7632), f1) & keep1};
-#pragma unroll
-                    for (int nt = 0; nt < NT; ++nt) mma16816(o[2 * blk + j][nt], a, pf[nt][0], pf[nt][1]);
-                  }
                 }
               }
             }
@@ -476,89 +526,139 @@ __global__ void __launch_bounds__(kWarps * 32, 2)
         stat_m[w][r] = f;
         sum = fmaf(stat_l[w][r], f, sum);
       }
-      joined_m[r] = top;
-      joined_l[r] = sum;
+      joined_m[r] = sum > 0.f ? top + log2f(sum) : sum == 0.f ? kNegInf : sum;
+      joined_l[r] = sum == 0.f ? 0.f : 1.f / sum;
     }
     __syncthreads();
 
-    const int c0 = split.cta_of(it.item_first), c1 = split.cta_of(it.item_first + it.item_units - 1);
+    const AttnSplit split = attn_split(p, tab);
+    const int c0 = split.cta_of(span[0]), c1 = split.cta_of(span[1]);
+    cur = span[2];
     auto write_out = [&](int r, int d, float v) {
-      const int tok = it.seq.q0 + i0 + r / p.group, h = it.head * p.group + r % p.group;
+      const int tok = it.seq.q0 + i0 + attn_token(p, r), h = it.head * p.group + r - attn_token(p, r) * p.group;
       p.out[(long long)tok * p.out_ld + (long long)h * D + d] = __float2half_rn(v);
     };
-    auto write_lse = [&](int r, float top, float sum) {
-      const int tok = it.seq.q0 + i0 + r / p.group, h = it.head * p.group + r % p.group;
-      if (p.lse) p.lse[(long long)tok * p.q_heads + h] = sum > 0.f ? (top + log2f(sum)) * 0.6931471805599453f : sum == 0.f ? kNegInf : sum;
+    auto write_lse = [&](int r, float stat) {
+      const int tok = it.seq.q0 + i0 + attn_token(p, r), h = it.head * p.group + r - attn_token(p, r) * p.group;
+      if (p.lse) p.lse[(long long)tok * p.q_heads + h] = stat * 0.6931471805599453f;
     };
-    const size_t slot_floats = (size_t)D * R + 2 * R;  // a multiple of four
-    float* slot = p.slots + (2 * (size_t)blockIdx.x + ((int)blockIdx.x == c0 ? 1 : 0)) * slot_floats;
+    constexpr size_t kSlot = D * R + R;  // floats of a partial result: O / l as [D][R], then m + log2 l
+    auto slot_of = [&](int cta) { return p.slots + (2 * (size_t)cta + (cta == c0 ? 1 : 0)) * kSlot; };
+    float* slot = slot_of(blockIdx.x);
+    const bool whole = c0 == c1;
+#pragma unroll 2
     for (int e = threadIdx.x; e < D * R; e += kWarps * 32) {
-      const int r = e % R, d = e / R;
+      const int r = e % R;
       float v = 0.f;
 #pragma unroll
       for (int w = 0; w < kWarps; ++w) v = fmaf(join[w * D * R + e], stat_m[w][r], v);
-      if (c0 == c1) {
-        if (r < rows) write_out(r, d, joined_l[r] == 0.f ? 0.f : v / joined_l[r]);
-      } else {
-        __stcg(slot + e, v);
-      }
+      v *= joined_l[r];
+      if (!whole) __stcg(slot + e, v);
+      else if (r < rows) write_out(r, e / R, v);
     }
-    if (c0 == c1) {
-      if (threadIdx.x < rows) write_lse(threadIdx.x, joined_m[threadIdx.x], joined_l[threadIdx.x]);
-    } else {
-      if (threadIdx.x < R) {
-        __stcg(slot + D * R + threadIdx.x, joined_m[threadIdx.x]);
-        __stcg(slot + D * R + R + threadIdx.x, joined_l[threadIdx.x]);
-      }
-      __threadfence();
-      __syncthreads();
-      if (threadIdx.x == 0) {
-        const unsigned before = atomicAdd(p.counters + c0, 1u);
-        is_last = before == (unsigned)(c1 - c0);
-        if (is_last) p.counters[c0] = 0;  // ready for the next call
-      }
-      __syncthreads();
-      if (is_last) {
+    if (threadIdx.x < R) {
+      if (!whole) __stcg(slot + D * R + threadIdx.x, joined_m[threadIdx.x]);
+      else if (threadIdx.x < rows) write_lse(threadIdx.x, joined_m[threadIdx.x]);
+    }
+    if (!whole) {
+      // The last CTA of each eight that share the item joins theirs in the place of the first of them;
+      // the last of those joins the eights. All loads of eight parts are in flight at once: a round
+      // trip to L2 is what each of the two steps takes.
+      const int parts = c1 - c0 + 1, eights = (parts + 7) / 8;
+      const int eight = (blockIdx.x - c0) / 8;
+      bool final = eights == 1;
+      int from = final ? c0 : c0 + 8 * eight, step = 1, n = final ? parts : min(8, c1 - from + 1);
+      // a CTA may be the first of an eight of two items: of one that it begins, and of one that it ends
+      unsigned* counter = p.counters + (final ? 0 : from == c0 ? 1 : 2) * kAttnMaxCtas + from;
+#pragma unroll 1
+      for (;;) {
         __threadfence();
-        // The parts' weights, [part][row] in shared memory, then the weighted
-        // sum in the parts' order: four rows of one column a thread, 16 bytes a part, eight parts'
-        // loads in flight.
-        const int parts = c1 - c0 + 1;
-        auto part = [&](int i) { return p.slots + (2 * (size_t)(c0 + i) + (i == 0 ? 1 : 0)) * slot_floats; };
-        for (int e = threadIdx.x; e < parts * R; e += kWarps * 32) join[e] = __ldcg(part(e / R) + D * R + e % R);
         __syncthreads();
-        for (int r = warp; r < R; r += kWarps) {
-          float top = kNegInf, sum = 0.f;
-          for (int i = lane; i < parts; i += 32) top = fmaxf(top, join[i * R + r]);
-#pragma unroll
-          for (int w = 16; w > 0; w >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, w));
-          for (int i = lane; i < parts; i += 32) {
-            const float f = top == kNegInf ? 0.f : ex2(join[i * R + r] - top);
-            join[i * R + r] = f;
-            sum = fmaf(__ldcg(part(i) + D * R + R + r), f, sum);
-          }
-#pragma unroll
-          for (int w = 16; w > 0; w >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, w);
-          if (lane == 0) {
-            joined_l[r] = sum;
-            if (r < rows) write_lse(r, top, sum);
-          }
+        if (threadIdx.x == 0) {
+          is_last = atomicAdd(counter, 1u) == (unsigned)(n - 1);
+          if (is_last) *counter = 0;  // ready for the next call
         }
         __syncthreads();
-        for (int e = 4 * threadIdx.x; e < D * R; e += 4 * kWarps * 32) {
-          const int r = e % R, d = e / R;
-          float v[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 8
-          for (int i = 0; i < parts; ++i) {
-            const float4 x = __ldcg(reinterpret_cast<const float4*>(part(i) + e));
-            const float4 f = *reinterpret_cast<const float4*>(join + i * R + r);
-            v[0] = fmaf(x.x, f.x, v[0]), v[1] = fmaf(x.y, f.y, v[1]);
-            v[2] = fmaf(x.z, f.z, v[2]), v[3] = fmaf(x.w, f.w, v[3]);
+        if (!is_last) break;
+        __threadfence();
+
+        constexpr int kCols = D * R / (4 * kWarps * 32) < 2 ? 1 : 2;  // of four rows, at a time
+#pragma unroll 1
+        for (int e0 = 4 * threadIdx.x; e0 < D * R; e0 += 4 * kWarps * 32 * kCols) {
+          float v[kCols][4];
+#pragma unroll
+          for (int k = 0; k < kCols; ++k) v[k][0] = v[k][1] = v[k][2] = v[k][3] = 0.f;
+          float top = kNegInf, total = 0.f;  // of row threadIdx.x
+#pragma unroll 1
+          for (int part0 = 0; part0 < n; part0 += 8) {
+            float4 x[kCols][8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              const float* part = slot_of(from + step * min(part0 + i, n - 1));
+#pragma unroll
+              for (int k = 0; k < kCols; ++k)
+                x[k][i] = __ldcg(reinterpret_cast<const float4*>(part + e0 + 4 * kWarps * 32 * k));
+            }
+            // weights[i][r], and in weights[8][r] what the sums so far are multiplied by
+            float* weights = join;
+            for (int i = threadIdx.x; i < 8 * R; i += kWarps * 32)
+              weights[i] = part0 + i / R < n ? __ldcg(slot_of(from + step * (part0 + i / R)) + D * R + i % R) : kNegInf;
+            __syncthreads();
+            if (threadIdx.x < R) {
+              float next = top;
+#pragma unroll
+              for (int i = 0; i < 8; ++i) next = fmaxf(next, weights[i * R + threadIdx.x]);
+              const float ref = next == kNegInf ? 0.f : next, old = ex2(top - ref);
+              total *= old;
+#pragma unroll
+              for (int i = 0; i < 8; ++i) {
+                const float f = ex2(weights[i * R + threadIdx.x] - ref);
+                weights[i * R + threadIdx.x] = f;
+                total += f;
+              }
+              weights[8 * R + threadIdx.x] = old;
+              joined_l[threadIdx.x] = total == 0.f ? 0.f : 1.f / total;
+              top = next;
+            }
+            __syncthreads();
+            const float* f = weights + e0 % R;
+            const float4 old = *reinterpret_cast<const float4*>(f + 8 * R);
+#pragma unroll
+            for (int k = 0; k < kCols; ++k) v[k][0] *= old.x, v[k][1] *= old.y, v[k][2] *= old.z, v[k][3] *= old.w;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              const float4 w = *reinterpret_cast<const float4*>(f + i * R);
+#pragma unroll
+              for (int k = 0; k < kCols; ++k) {
+                v[k][0] = fmaf(x[k][i].x, w.x, v[k][0]), v[k][1] = fmaf(x[k][i].y, w.y, v[k][1]);
+                v[k][2] = fmaf(x[k][i].z, w.z, v[k][2]), v[k][3] = fmaf(x[k][i].w, w.w, v[k][3]);
+              }
+            }
+            __syncthreads();  // the weights' places are used again
           }
 #pragma unroll
-          for (int k = 0; k < 4; ++k)
-            if (r + k < rows) write_out(r + k, d, joined_l[r + k] == 0.f ? 0.f : v[k] / joined_l[r + k]);
+          for (int k = 0; k < kCols; ++k) {
+            const int e = e0 + 4 * kWarps * 32 * k, r = e % R;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[k][j] *= joined_l[r + j];
+            if (!final) {  // only this thread reads here
+              __stcg(reinterpret_cast<float4*>(slot_of(from) + e), make_float4(v[k][0], v[k][1], v[k][2], v[k][3]));
+            } else {
+#pragma unroll
+              for (int j = 0; j < 4; ++j)
+                if (r + j < rows) write_out(r + j, e / R, v[k][j]);
+            }
+          }
+          if (threadIdx.x < R)
+            joined_m[threadIdx.x] = total > 0.f ? top + log2f(total) : total == 0.f ? kNegInf : total;
         }
+        __syncthreads();
+        if (threadIdx.x < R) {
+          if (!final) __stcg(slot_of(from) + D * R + threadIdx.x, joined_m[threadIdx.x]);
+          else if (threadIdx.x < rows) write_lse(threadIdx.x, joined_m[threadIdx.x]);
+        }
+        if (final) break;
+        final = true, from = c0, step = 8, n = eights, counter = p.counters + c0;
       }
     }
     // the next item's copies write where these reads and writes were
@@ -568,11 +668,11 @@ __global__ void __launch_bounds__(kWarps * 32, 2)
 }
 
 template <int FMT, int D, int NT>
-cudaError_t launch(const qtea_kv* kv, const AttnParams& p, int grid, cudaStream_t st) {
+cudaError_t launch(const qtea_kv* kv, const AttnParams& p, cudaStream_t st) {
   using T = Rows<FMT, D, NT>;
-  const int smem = T::kRing + T::kScaleRing;
-  static_assert(kWarps * D * 8 * NT * 4 <= T::kRing && kRowsGrid * 8 * NT * 4 <= T::kRing,
-                "what is joined fits the rings");
+  const int smem = T::kRing + T::kScaleRing + kAttnTableBytes(p.b.n_seqs);
+  const int grid = std::min(T::kCtas * kv->sm_count, kAttnMaxCtas);
+  static_assert(kWarps * D * 8 * NT * 4 <= T::kRing, "the joined results fit the rings");
   auto k = qtea_attn_rows_kernel<FMT, D, NT>;
   cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   if (e != cudaSuccess) return e;
@@ -581,35 +681,36 @@ cudaError_t launch(const qtea_kv* kv, const AttnParams& p, int grid, cudaStream_
 }
 
 template <int FMT, int D>
-cudaError_t launch_nt(const qtea_kv* kv, const AttnParams& p, int nt, int grid, cudaStream_t st) {
-  if (nt == 1) return launch<FMT, D, 1>(kv, p, grid, st);
-  if (nt == 2) return launch<FMT, D, 2>(kv, p, grid, st);
-  return launch<FMT, D, 4>(kv, p, grid, st);
+cudaError_t launch_nt(const qtea_kv* kv, const AttnParams& p, int nt, cudaStream_t st) {
+  if (nt == 1) return launch<FMT, D, 1>(kv, p, st);
+  if (nt == 2) return launch<FMT, D, 2>(kv, p, st);
+  return launch<FMT, D, 4>(kv, p, st);
 }
 
 template <int FMT>
-cudaError_t launch_dim(const qtea_kv* kv, const AttnParams& p, int nt, int grid, cudaStream_t st) {
-  return kv->view.dim == 128 ? launch_nt<FMT, 128>(kv, p, nt, grid, st) : launch_nt<FMT, 64>(kv, p, nt, grid, st);
+cudaError_t launch_dim(const qtea_kv* kv, const AttnParams& p, int nt, cudaStream_t st) {
+  return kv->view.dim == 128 ? launch_nt<FMT, 128>(kv, p, nt, st) : launch_nt<FMT, 64>(kv, p, nt, st);
 }
 
 }  // namespace
 
-int attn_rows_grid(int sm_count) { return std::min(2 * sm_count, kRowsGrid); }
-
-size_t attn_rows_floats(int sm_count) { return (size_t)attn_rows_grid(sm_count) * (128 * kMaxRows + 2 * kMaxRows); }
+size_t attn_rows_floats(int sm_count) {  // two CTAs of 32 rows an SM, or three of 8
+  return (size_t)2 * sm_count * (128 * kMaxRows + 2 * kMaxRows);
+}
 
 cudaError_t launch_attn_rows(const qtea_kv* kv, const AttnParams& base, cudaStream_t st) {
   AttnParams p = base;
-  const int grid = attn_rows_grid(kv->sm_count);
   // column tiles of 8 rows: the fewest that hold the longest sequence's rows, or whole tokens at 32
   const long long rows = (long long)p.group * p.b.max_q;
   const int nt = rows <= 8 ? 1 : rows <= 16 ? 2 : 4;
   p.tile_tokens = 8 * nt / p.group;
-  p.unit_shift = kv->view.format == QTEA_KV_F16 ? 4 : kv->view.format == QTEA_KV_FP8 ? 5 : 6;
-  p.min_units = 2 * kWarps;
-  if (kv->view.format == QTEA_KV_F16) return launch_dim<QTEA_KV_F16>(kv, p, nt, grid, st);
-  if (kv->view.format == QTEA_KV_FP8) return launch_dim<QTEA_KV_FP8>(kv, p, nt, grid, st);
-  return launch_dim<QTEA_KV_FP4>(kv, p, nt, grid, st);
+  p.unit_shift = kv_unit_shift(kv->view.format);
+  p.item_cost = kv->view.format == QTEA_KV_F16 ? 16 : 8;
+  p.min_units = kv->view.format == QTEA_KV_F16 ? 24 : 12;
+  if (!attn_cost_fits(p)) return cudaErrorInvalidValue;
+  if (kv->view.format == QTEA_KV_F16) return launch_dim<QTEA_KV_F16>(kv, p, nt, st);
+  if (kv->view.format == QTEA_KV_FP8) return launch_dim<QTEA_KV_FP8>(kv, p, nt, st);
+  return launch_dim<QTEA_KV_FP4>(kv, p, nt, st);
 }
 
 }  // namespace qtea
@@ -662,6 +763,7 @@ int qtea_attention(const qtea_kv* kv, const qtea_kv_batch* batch, const uint16_t
   p.lse = lse;
   p.q_ld = q_ld, p.out_ld = out_ld;
   p.q_heads = n_q_heads;
+  p.group_inverse = (65536u + p.group - 1) / p.group;
   p.scale_log2 = scale * 1.4426950408889634f;
   p.window = window;
   p.status = static_cast<int*>(workspace);
@@ -669,7 +771,9 @@ int qtea_attention(const qtea_kv* kv, const qtea_kv_batch* batch, const uint16_t
   p.slots = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + kAttnHeaderBytes);
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
   const bool few = (long long)p.group * p.b.max_q <= kMaxRows;
-  if ((few ? launch_attn_rows(kv, p, st) : launch_attn_chunk(kv, p, st)) != cudaSuccess) {
+  const cudaError_t e = few ? launch_attn_rows(kv, p, st) : launch_attn_chunk(kv, p, st);
+  if (e == cudaErrorInvalidValue) return QTEA_ERR_UNSUPPORTED;
+  if (e != cudaSuccess) {
     cudaGetLastError();
     return QTEA_ERR_CUDA;
   }

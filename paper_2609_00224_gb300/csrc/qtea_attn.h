@@ -3,7 +3,8 @@
 // The work of a call is a sequence of units: for every sequence, cache head and tile of query rows
 // (an item), the stretches of unit_keys keys that the tile sees. The grid's CTAs take equal runs of
 // that sequence, whatever the lengths are, so a ragged batch loads every SM alike and a single long
-// sequence is split over all of them. An item that several CTAs share is joined by the last of them
+// sequence is split over all of them; each item counts for a few units more than it has, for what it
+// costs beside them. An item that several CTAs share is joined by the last of them
 // to finish: the others leave (O, m, l) in the workspace. Which CTAs share an item follows from
 // the unit numbers alone, and they are joined in that order, so results do not depend on timing.
 #pragma once
@@ -12,8 +13,8 @@
 
 namespace qtea {
 
-constexpr int kAttnHeaderBytes = 8192;  // workspace: the status word, then one counter per CTA
-constexpr int kAttnCounters = 1024;     // at most this many CTAs
+constexpr int kAttnMaxCtas = 1024;
+constexpr int kAttnHeaderBytes = 16384;  // workspace: the status word, then three counters per CTA
 constexpr int kAttnMaxGroup = 32;       // query heads of one cache head
 
 struct AttnParams {
@@ -24,13 +25,15 @@ struct AttnParams {
   float* lse;
   long long q_ld, out_ld;
   int q_heads, group;
+  unsigned group_inverse;  // ceil(2^16 / group)
   float scale_log2;  // scale * log2(e)
   int window;
   int tile_tokens;  // tokens of an item: the rows of a tile / group
   int unit_shift;   // log2 of a unit's keys
-  int min_units;    // the least units worth a CTA of their own
+  int item_cost;    // what an item costs beside its units, in units
+  int min_units;    // the least cost worth a CTA of its own
   int* status;
-  unsigned* counters;
+  unsigned* counters;  // [3][kAttnMaxCtas]
   float* slots;     // [grid][2] partial results
 };
 
@@ -39,6 +42,17 @@ size_t attn_chunk_floats(int sm_count);  // of one partial result for each CTA
 cudaError_t launch_attn_rows(const qtea_kv* kv, const AttnParams& p, cudaStream_t st);
 size_t attn_rows_floats(int sm_count);  // of one partial result for each CTA
 
+// Bytes of the batch's table in shared memory (AttnTable).
+constexpr int kAttnTableBytes(int n_seqs) { return 4 * (n_seqs + 1) + 12 * n_seqs; }
+
+// Whether the cost of any batch of these sizes fits 31 bits, once tile_tokens, unit_shift and item_cost
+// are set: every sequence's tiles with all the keys that its page table can name.
+inline bool attn_cost_fits(const AttnParams& p) {
+  const double tiles = (double)p.b.n_tokens / p.tile_tokens + p.b.n_seqs;
+  const double units = (double)p.b.max_pages * p.kv.page_size / (1 << p.unit_shift) + p.item_cost + 1;
+  return tiles * units * p.kv.heads < 2147483648.0;
+}
+
 #ifdef __CUDACC__
 
 // One sequence of the batch.
@@ -46,14 +60,30 @@ struct AttnSeq {
   int q0, n, base;  // first row, new tokens, position of the first
 };
 
+// The batch in a CTA's shared memory: every sequence, and the cost units before it.
+struct AttnTable {
+  int* prefix;   // [n_seqs + 1]
+  AttnSeq* seq;  // [n_seqs]
+};
+__device__ __forceinline__ AttnTable attn_table(void* memory, int n_seqs) {
+  AttnTable t;
+  t.prefix = static_cast<int*>(memory);
+  t.seq = reinterpret_cast<AttnSeq*>(t.prefix + n_seqs + 1);
+  return t;
+}
+
 __device__ __forceinline__ AttnSeq attn_seq(const AttnParams& p, int s) {
   AttnSeq a;
-  a.q0 = min(max(__ldg(p.b.q_start + s), 0), p.b.n_tokens);
-  const int q1 = min(max(__ldg(p.b.q_start + s + 1), a.q0), p.b.n_tokens);
-  a.base = kv_context(p.b, p.kv, s) - (q1 - a.q0);
-  a.n = min(q1 - a.q0, p.b.max_q);
+  const int q0 = __ldg(p.b.q_start + s), q1 = __ldg(p.b.q_start + s + 1), ctx = kv_context(p.b, p.kv, s);
+  a.q0 = min(max(q0, 0), p.b.n_tokens);
+  const int n = min(max(q1, a.q0), p.b.n_tokens) - a.q0;
+  a.base = ctx - n;
+  a.n = min(n, p.b.max_q);
   return a;
 }
+
+// r / group for a row of a tile: exact for r < 256 and group <= 32.
+__device__ __forceinline__ int attn_token(const AttnParams& p, int r) { return (int)((unsigned)r * p.group_inverse >> 16); }
 
 // The units of tile t of a sequence: first unit and their number (at least one, for tiles that see
 // nothing have zeros to write).
@@ -70,57 +100,66 @@ __device__ __forceinline__ int attn_tiles(const AttnParams& p, const AttnSeq& a)
   return (a.n + p.tile_tokens - 1) / p.tile_tokens;
 }
 
-// Units before each sequence, into shared memory: prefix[0 .. n_seqs] (every thread of the CTA
-// calls it; it ends with a barrier).
-__device__ __forceinline__ void attn_prefix(const AttnParams& p, long long* prefix) {
+// Fills the table (every thread of the CTA calls it; it ends with a barrier). An item costs its
+// units and item_cost more, which stand before them.
+__device__ __forceinline__ void attn_prefix(const AttnParams& p, const AttnTable& tab) {
   const int n = p.b.n_seqs, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   if (p.b.max_q <= p.tile_tokens) {  // one tile a sequence: a thread each
     for (int s = threadIdx.x; s < n; s += blockDim.x) {
       const AttnSeq a = attn_seq(p, s);
-      prefix[s + 1] = a.n > 0 ? (long long)attn_tile(p, a, 0).y * p.kv.heads : 0;
+      tab.seq[s] = a;
+      tab.prefix[s + 1] = a.n > 0 ? (attn_tile(p, a, 0).y + p.item_cost) * p.kv.heads : 0;
     }
   } else {  // a warp each
     for (int s = warp; s < n; s += blockDim.x >> 5) {
       const AttnSeq a = attn_seq(p, s);
       const int tiles = attn_tiles(p, a);
-      long long sum = 0;
-      for (int t = lane; t < tiles; t += 32) sum += attn_tile(p, a, t).y;
+      int sum = 0;
+      for (int t = lane; t < tiles; t += 32) sum += attn_tile(p, a, t).y + p.item_cost;
 #pragma unroll
       for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-      if (lane == 0) prefix[s + 1] = sum * p.kv.heads;
+      if (lane == 0) {
+        tab.seq[s] = a;
+        tab.prefix[s + 1] = sum * p.kv.heads;
+      }
     }
   }
   __syncthreads();
   if (warp == 0) {
-    long long before = 0;
-    if (lane == 0) prefix[0] = 0;
+    int before = 0;
+    if (lane == 0) tab.prefix[0] = 0;
     for (int s0 = 0; s0 < n; s0 += 32) {
-      long long v = s0 + lane < n ? prefix[s0 + lane + 1] : 0;
+      int v = s0 + lane < n ? tab.prefix[s0 + lane + 1] : 0;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
-        const long long u = __shfl_up_sync(0xffffffffu, v, o);
+        const int u = __shfl_up_sync(0xffffffffu, v, o);
         if (lane >= o) v += u;
       }
-      if (s0 + lane < n) prefix[s0 + lane + 1] = before + v;
+      if (s0 + lane < n) tab.prefix[s0 + lane + 1] = before + v;
       before += __shfl_sync(0xffffffffu, v, 31);
     }
   }
   __syncthreads();
 }
 
-// How the units are divided: CTA c of `ctas` takes [first(c), first(c + 1)).
+// How the cost is divided: CTA c of `ctas` takes [first(c), first(c + 1)), the first `more` of them
+// one unit more than the others. (The host has checked that all fit 31 bits.)
 struct AttnSplit {
-  long long total;
-  int ctas;
-  __device__ __forceinline__ long long first(int c) const { return total * c / ctas; }
-  __device__ __forceinline__ int cta_of(long long u) const { return (int)(((u + 1) * ctas - 1) / total); }
+  int total, each, ctas, more;
+  __device__ __forceinline__ int first(int c) const { return each * c + min(c, more); }
+  __device__ __forceinline__ int cta_of(int u) const {
+    const int wide = (each + 1) * more;
+    return u < wide ? (int)((unsigned)u / (unsigned)(each + 1)) : more + (int)((unsigned)(u - wide) / (unsigned)each);
+  }
 };
 
-__device__ __forceinline__ AttnSplit attn_split(const AttnParams& p, const long long* prefix) {
+__device__ __forceinline__ AttnSplit attn_split(const AttnParams& p, const AttnTable& tab) {
   AttnSplit d;
-  d.total = prefix[p.b.n_seqs];
-  const long long worth = (d.total + p.min_units - 1) / p.min_units;
-  d.ctas = (int)min((long long)gridDim.x, max(worth, 1LL));
+  d.total = tab.prefix[p.b.n_seqs];
+  const unsigned worth = ((unsigned)d.total + p.min_units - 1) / (unsigned)p.min_units;
+  d.ctas = (int)min(gridDim.x, max(worth, 1u));
+  d.each = (int)((unsigned)d.total / (unsigned)d.ctas);
+  d.more = d.total - d.each * d.ctas;
   return d;
 }
 
@@ -128,39 +167,45 @@ __device__ __forceinline__ AttnSplit attn_split(const AttnParams& p, const long 
 struct AttnItem {
   AttnSeq seq;
   int s, head, tile;
-  int unit0;            // the stretch's first unit, in units from the start of the sequence's keys
-  int units;            // its units
-  long long item_first; // number of the item's first unit in the call
-  int item_units;       // all of the item's units
+  int unit0;             // the stretch's first unit, in units from the start of the sequence's keys
+  int units;             // its units; none where the stretch is part of the item's fixed cost only
+  int first, last;       // the cost numbers of the item's first and last units
+  int next;              // where the stretch after this one begins
 };
 
-// The item that holds unit `cur`, and the part of it in [cur, end). Every lane of a warp calls it.
-__device__ __forceinline__ AttnItem attn_item(const AttnParams& p, const long long* prefix, long long cur,
-                                              long long end) {
+// The stretch of one item that begins at cost number `cur` of a run that ends at `end`. Every lane
+// of a warp calls it.
+__device__ __forceinline__ AttnItem attn_item(const AttnParams& p, const AttnTable& tab, int cur, int end) {
   AttnItem it;
   int lo = 0, hi = p.b.n_seqs;
-  while (hi - lo > 1) {  // the last sequence whose units start at or before cur (it is not empty)
+  while (hi - lo > 1) {  // the last sequence whose cost starts at or before cur (it is not empty)
     const int mid = (lo + hi) >> 1;
-    if (prefix[mid] <= cur) lo = mid;
+    if (tab.prefix[mid] <= cur) lo = mid;
     else hi = mid;
   }
   it.s = lo;
-  it.seq = attn_seq(p, lo);
-  const long long per_head = (prefix[lo + 1] - prefix[lo]) / p.kv.heads;
-  const long long in_seq = cur - prefix[lo];
-  it.head = (int)(in_seq / per_head);
-  long long rem = in_seq - it.head * per_head;
-  int2 u = attn_tile(p, it.seq, 0);
-  it.tile = 0;
-  if (p.b.max_q > p.tile_tokens) {
+  it.seq = tab.seq[lo];
+  const int in_seq = cur - tab.prefix[lo];
+  int2 u;
+  int rem;  // from the item's start
+  if (p.b.max_q <= p.tile_tokens) {
+    u = attn_tile(p, it.seq, 0);
+    it.tile = 0;
+    it.head = (int)((unsigned)in_seq / (unsigned)(u.y + p.item_cost));
+    rem = in_seq - it.head * (u.y + p.item_cost);
+  } else {
+    const int per_head = (int)((unsigned)(tab.prefix[lo + 1] - tab.prefix[lo]) / (unsigned)p.kv.heads);
+    it.head = (int)((unsigned)in_seq / (unsigned)per_head);
+    rem = in_seq - it.head * per_head;
     const int lane = threadIdx.x & 31, tiles = attn_tiles(p, it.seq);
     for (int t0 = 0;; t0 += 32) {
       const int t = t0 + lane;
-      const int2 mine = t < tiles ? attn_tile(p, it.seq, t) : make_int2(0, 0);
-      long long v = mine.y;
+      int2 mine = make_int2(0, 0);
+      if (t < tiles) mine = attn_tile(p, it.seq, t), mine.y += p.item_cost;
+      int v = mine.y;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
-        const long long w = __shfl_up_sync(0xffffffffu, v, o);
+        const int w = __shfl_up_sync(0xffffffffu, v, o);
         if (lane >= o) v += w;
       }
       const unsigned past = __ballot_sync(0xffffffffu, v > rem);
@@ -170,15 +215,18 @@ __device__ __forceinline__ AttnItem attn_item(const AttnParams& p, const long lo
         u.x = __shfl_sync(0xffffffffu, mine.x, at);
         u.y = __shfl_sync(0xffffffffu, mine.y, at);
         rem -= __shfl_sync(0xffffffffu, v, at) - u.y;
+        u.y -= p.item_cost;
         break;
       }
       rem -= __shfl_sync(0xffffffffu, v, 31);
     }
   }
-  it.item_first = cur - rem;
-  it.item_units = u.y;
-  it.unit0 = u.x + (int)rem;
-  it.units = (int)min((long long)(u.y - rem), end - cur);
+  it.first = cur - rem + p.item_cost;
+  it.last = it.first + u.y - 1;
+  it.next = min(it.last + 1, end);
+  const int from = max(cur, it.first);
+  it.unit0 = u.x + from - it.first;
+  it.units = max(it.next - from, 0);
   return it;
 }
 #endif

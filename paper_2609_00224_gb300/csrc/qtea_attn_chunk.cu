@@ -16,7 +16,7 @@
 //    and the accumulator rescaled. Until then a thread holds 64 registers of weights; over a
 //    quantised cache the converting warps need those registers, so there the maximum is looked for
 //    first, in a second reading of S, and the reference follows it by at most 2^8;
-//  * one warp issues every product, one warp every copy; keys and values are boxes of 16 tokens
+//  * one warp issues every product, one warp every copy; keys and values are boxes of a page,
 //    swizzled on the way into shared memory. K is the second operand K-major, V is taken MN-major, so
 //    neither is transposed. Quantised rows are copied as they are into a ring of their own, and four
 //    warps write them as fp16 (exactly) in the same swizzled form.
@@ -200,7 +200,6 @@ struct Chunk {
 };
 
 struct ChunkShared {
-  long long prefix[kKvMaxSeqs + 1];
   uint64_t full[8], empty[8];          // stages of K and V
   uint64_t raw_full[6], raw_empty[6];  // stages of quantised rows
   uint64_t q_full, q_empty, o_free;
@@ -282,10 +281,11 @@ __global__ void __launch_bounds__((Chunk<FMT, D>::kThreads), 1)
     }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  attn_prefix(p, sh.prefix);  // ends with a barrier
-  const AttnSplit split = attn_split(p, sh.prefix);
+  const AttnTable tab = attn_table(smem_raw + T::kSmem, p.b.n_seqs);
+  attn_prefix(p, tab);  // ends with a barrier
+  const AttnSplit split = attn_split(p, tab);
   if (split.total == 0 || (int)blockIdx.x >= split.ctas) return;
-  const long long begin = split.first(blockIdx.x), end = split.first(blockIdx.x + 1);
+  const int begin = split.first(blockIdx.x), end = split.first(blockIdx.x + 1);
   if (warp == T::kMmaWarp) tmem_alloc(smem_u32(&sh.tmem), 512);
   tmem_fence_before();
   __syncthreads();
@@ -302,10 +302,12 @@ __global__ void __launch_bounds__((Chunk<FMT, D>::kThreads), 1)
     
     if (warp == T::kCopyWarp) {
       // ------------------------------------------------------------------ copies of keys and values
+      const int box = min(p.kv.page_size, kUnit), boxes = kUnit / box;  // tokens of a copy, copies of a unit
       uint32_t stage = 0, phase = 1;  // the first wait of every stage passes
-      for (long long cur = begin; cur < end;) {
-        const AttnItem it = attn_item(p, sh.prefix, cur, end);
-        cur += it.units;
+      for (int cur = begin; cur < end;) {
+        const AttnItem it = attn_item(p, tab, cur, end);
+        cur = it.next;
+        if (it.units == 0) continue;
         const int* pages = p.b.pages + (long long)it.s * p.b.max_pages;
         const Order order{it.units, cp.two};
         for (int i = 0; i < order.steps(); ++i) {
@@ -313,8 +315,8 @@ __global__ void __launch_bounds__((Chunk<FMT, D>::kThreads), 1)
           bool value;
           order.at(i, &unit, &value);
           int row = 0;
-          if (lane < 8) {
-            const int key = (it.unit0 + unit) * kUnit + 16 * lane;
+          if (lane < boxes) {
+            const int key = (it.unit0 + unit) * kUnit + box * lane;
             const int page = __ldg(pages + min(key >> p.kv.page_shift, p.b.max_pages - 1));
             row = (min(max(page, 0), p.kv.n_pages - 1) * p.kv.heads + it.head) * p.kv.page_size +
                   (key & (p.kv.page_size - 1));
@@ -323,15 +325,15 @@ __global__ void __launch_bounds__((Chunk<FMT, D>::kThreads), 1)
           const uint32_t bar = smem_u32(T::kQuant ? &sh.raw_full[stage] : &sh.full[stage]);
           if (lane == 0) mbar_arrive_expect_tx(bar, T::kQuant ? T::kRawBytes : T::kTileBytes);
           __syncwarp();
-          if (lane < 8) {
+          if (lane < boxes) {
             if (T::kQuant) {
               const uint32_t dst = raw_smem + stage * T::kRawBytes;
-              bulk_load(dst + lane * 16 * T::kRawRow, (value ? p.kv.v : p.kv.k) + (long long)row * T::kRawRow,
-                        16 * T::kRawRow, bar);
-              bulk_load(dst + kUnit * T::kRawRow + lane * 16 * T::kScaleRow,
-                        (value ? p.kv.vs : p.kv.ks) + (long long)row * T::kScaleRow, 16 * T::kScaleRow, bar);
+              bulk_load(dst + lane * box * T::kRawRow, (value ? p.kv.v : p.kv.k) + (long long)row * T::kRawRow,
+                        box * T::kRawRow, bar);
+              bulk_load(dst + kUnit * T::kRawRow + lane * box * T::kScaleRow,
+                        (value ? p.kv.vs : p.kv.ks) + (long long)row * T::kScaleRow, box * T::kScaleRow, bar);
             } else {
-              const uint32_t dst = kv_smem + stage * T::kTileBytes + lane * 2048;
+              const uint32_t dst = kv_smem + stage * T::kTileBytes + lane * box * 128;
 #pragma unroll
               for (int h = 0; h < T::kParts; ++h)
                 tma_load_2d(dst + h * T::kPartBytes, value ? &map_v : &map_k, h * 128, row, bar);
@@ -346,9 +348,10 @@ __global__ void __launch_bounds__((Chunk<FMT, D>::kThreads), 1)
       constexpr uint32_t kIdescO = 1u << 4 | 1u << 16 | (D >> 3) << 17 | (kRowsTile >> 4) << 24;
       uint32_t stage = 0, phase = 0;
       uint32_t q_phase = 0, o_phase = 1, p_phase[2] = {0, 0};
-      for (long long cur = begin; cur < end;) {
-        const AttnItem it = attn_item(p, sh.prefix, cur, end);
-        cur += it.units;
+      for (int cur = begin; cur < end;) {
+        const AttnItem it = attn_item(p, tab, cur, end);
+        cur = it.next;
+        if (it.units == 0) continue;
         const Bounds in = item_bounds(p, it);
         const int n = it.units;
         const bool second = cp.two && it.seq.n - it.tile * p.tile_tokens > cp.half_tokens;
@@ -464,9 +467,10 @@ __global__ void __launch_bounds__((Chunk<FMT, D>::kThreads), 1)
     } else if (warp == T::kQWarp) {
       // ----------------------------------------------------------------------------------- queries
       uint32_t q_phase = 1;
-      for (long long cur = begin; cur < end;) {
-        const AttnItem it = attn_item(p, sh.prefix, cur, end);
-        cur += it.units;
+      for (int cur = begin; cur < end;) {
+        const AttnItem it = attn_item(p, tab, cur, end);
+        cur = it.next;
+        if (it.units == 0) continue;
         const int i0 = it.tile * p.tile_tokens, tokens = min(it.seq.n - i0, p.tile_tokens);
         const int tiles = cp.two && tokens > cp.half_tokens ? 2 : 1;
         if (!wait(sh.q_empty, q_phase)) break;
@@ -487,8 +491,8 @@ __global__ void __launch_bounds__((Chunk<FMT, D>::kThreads), 1)
             for (int i = lane; i < rows * (D / 8); i += 32) {
               const int r = i / (D / 8), ch = i % (D / 8);
               const uint32_t* from = reinterpret_cast<const uint32_t*>(
-                  p.q + (long long)(it.seq.q0 + i0 + t * cp.half_tokens + r / p.group) * p.q_ld +
-                  (long long)(it.head * p.group + r % p.group) * D + ch * 8);
+                  p.q + (long long)(it.seq.q0 + i0 + t * cp.half_tokens + attn_token(p, r)) * p.q_ld +
+                  (long long)(it.head * p.group + (r - attn_token(p, r) * p.group)) * D + ch * 8);
               sts128(q_smem + t * T::kTileBytes + (ch >> 3) * T::kPartBytes + r * 128 + (((ch & 7) ^ (r & 7)) << 4),
                      make_uint4(from[0] ^ cp.q_flip, from[1] ^ cp.q_flip, from[2] ^ cp.q_flip, from[3] ^ cp.q_flip));
             }
@@ -503,9 +507,10 @@ __global__ void __launch_bounds__((Chunk<FMT, D>::kThreads), 1)
     // ------------------------------------------------------------------ quantised rows to fp16 tiles
     const int tid = threadIdx.x - 256;
     uint32_t stage = 0, phase = 1, raw = 0, raw_phase = 0;
-    for (long long cur = begin; cur < end;) {
-      const AttnItem it = attn_item(p, sh.prefix, cur, end);
-      cur += it.units;
+    for (int cur = begin; cur < end;) {
+      const AttnItem it = attn_item(p, tab, cur, end);
+      cur = it.next;
+      if (it.units == 0) continue;
       const Bounds in = item_bounds(p, it);
       const Order order{it.units, cp.two};
       for (int i = 0; i < order.steps() && ok; ++i) {
@@ -569,18 +574,19 @@ __global__ void __launch_bounds__((Chunk<FMT, D>::kThreads), 1)
     const uint32_t lanes = tmem + ((uint32_t)(warp & 3) << 21);  // this warp's 32 lanes
     const uint32_t s_addr = lanes + g * 128, o_addr = lanes + 256 + g * 128;
     uint32_t s_phase = 0, o_phase = 0, odd = 0;
-    for (long long cur = begin, next = begin; cur < end; cur = next) {
+    for (int cur = begin, next = begin; cur < end; cur = next) {
       int unit0, n, steps, hi, lo, hi_in, lo_in;
       bool live;  // a row of the item (the tile may have others, and its lanes then hold anything)
       {
-        const AttnItem it = attn_item(p, sh.prefix, cur, end);
-        next = cur + it.units;
+        const AttnItem it = attn_item(p, tab, cur, end);
+        next = it.next;
+        if (it.units == 0) continue;
         n = it.units, unit0 = it.unit0;
         const int t0 = it.tile * p.tile_tokens + (cp.two ? g * cp.half_tokens : 0);
         const int tokens = max(0, min(min(it.seq.n - t0, cp.half_tokens), p.tile_tokens));
         live = row < tokens * p.group;
         steps = cp.two ? (tokens > 0 ? n : 0) : (n + 1 - g) >> 1;
-        const int first = it.seq.base + t0, last = first + tokens - 1, pos = first + row / p.group;
+        const int first = it.seq.base + t0, last = first + tokens - 1, pos = first + attn_token(p, row);
         hi = pos + 1, lo = p.window > 0 ? max(0, pos - p.window + 1) : 0;
         // keys that all of the group's rows see: units inside need no mask
         hi_in = first + 1, lo_in = p.window > 0 ? max(0, last - p.window + 1) : 0;
@@ -696,9 +702,9 @@ __global__ void __launch_bounds__((Chunk<FMT, D>::kThreads), 1)
       if (!cp.two && g == 1) sh.m1[odd][row] = m, sh.l1[odd][row] = l;
       named_barrier<1>(256);
       tmem_fence_after();
-      const AttnItem it = attn_item(p, sh.prefix, cur, end);  // again: not kept over the loop above
+      const AttnItem it = attn_item(p, tab, cur, end);  // again: not kept over the loop above
       const int t0 = it.tile * p.tile_tokens + (cp.two ? g * cp.half_tokens : 0);
-      const int c0 = split.cta_of(it.item_first), c1 = split.cta_of(it.item_first + it.item_units - 1);
+      const int c0 = split.cta_of(it.first), c1 = split.cta_of(it.last);
       // With one row tile the first group joins both accumulators (the lanes are the same).
       const bool writer = cp.two ? true : g == 0;
       float fa = 1.f, fb = 0.f;
@@ -710,7 +716,7 @@ __global__ void __launch_bounds__((Chunk<FMT, D>::kThreads), 1)
         l = l * fa + l1 * fb;
       }
       const bool both = !cp.two && n > 1;
-      const int tok = it.seq.q0 + t0 + row / p.group, head = it.head * p.group + row % p.group;
+      const int tok = it.seq.q0 + t0 + attn_token(p, row), head = it.head * p.group + (row - attn_token(p, row) * p.group);
       const bool mine = writer && live;
       constexpr size_t kSlot = (size_t)2 * kRowsTile * (128 + 2);  // floats: [D/4][256][4], then m, l
       float* slot = p.slots + (2 * (size_t)blockIdx.x + ((int)blockIdx.x == c0 ? 1 : 0)) * kSlot;
@@ -828,11 +834,12 @@ __global__ void __launch_bounds__((Chunk<FMT, D>::kThreads), 1)
 template <int FMT, int D>
 cudaError_t launch(const qtea_kv* kv, const ChunkParams& cp, const CUtensorMap& map_q, cudaStream_t st) {
   using T = Chunk<FMT, D>;
-  static_assert(T::kSmem + sizeof(ChunkShared) <= 227 * 1024, "shared memory of a CTA");
+  static_assert(T::kSmem + kAttnTableBytes(kKvMaxSeqs) + sizeof(ChunkShared) <= 227 * 1024, "shared memory of a CTA");
+  const int smem = T::kSmem + kAttnTableBytes(cp.a.b.n_seqs);
   auto k = qtea_attn_chunk_kernel<FMT, D>;
-  cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, T::kSmem);
+  cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   if (e != cudaSuccess) return e;
-  k<<<std::min(kv->sm_count, kAttnCounters), T::kThreads, T::kSmem, st>>>(kv->map_k, kv->map_v, map_q, cp);
+  k<<<std::min(kv->sm_count, kAttnMaxCtas), T::kThreads, smem, st>>>(kv->wide_k, kv->wide_v, map_q, cp);
   return cudaGetLastError();
 }
 
@@ -844,7 +851,7 @@ cudaError_t launch_dim(const qtea_kv* kv, const ChunkParams& cp, const CUtensorM
 }  // namespace
 
 size_t attn_chunk_floats(int sm_count) {
-  return (size_t)std::min(sm_count, kAttnCounters) * 2 * kRowsTile * (128 + 2);
+  return (size_t)std::min(sm_count, kAttnMaxCtas) * 2 * kRowsTile * (128 + 2);
 }
 
 cudaError_t launch_attn_chunk(const qtea_kv* kv, const AttnParams& base, cudaStream_t st) {
@@ -856,7 +863,9 @@ cudaError_t launch_attn_chunk(const qtea_kv* kv, const AttnParams& base, cudaStr
   cp.two = p.b.max_q > cp.half_tokens;
   p.tile_tokens = cp.two ? 2 * cp.half_tokens : cp.half_tokens;
   p.unit_shift = 7;
-  p.min_units = 2;
+  p.item_cost = 2;
+  p.min_units = 3;
+  if (!attn_cost_fits(p)) return cudaErrorInvalidValue;
   const bool negative = p.scale_log2 < 0.f;
   cp.q_flip = negative ? 0x80008000u : 0u;
   // a masked score is -infinity before it is scaled: a scale of zero becomes one that is zero in effect

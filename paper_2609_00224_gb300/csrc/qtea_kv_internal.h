@@ -8,7 +8,7 @@
 namespace qtea {
 
 constexpr int kKvBlock = 32;      // elements that share a power of two
-constexpr int kKvMaxSeqs = 1024;  // sequences of one call
+constexpr int kKvMaxSeqs = 512;   // sequences of one call: their table lies in shared memory
 constexpr int kKvEMin = -14;      // every value is then a multiple of 2^-23: exact in fp16
 constexpr int kKvEMaxFp8 = 7;     // 448 * 2^7 = 57344
 constexpr int kKvEMaxFp4 = 13;    // 6 * 2^13 = 49152
@@ -123,5 +123,14 @@ struct qtea_kv {
   qtea::KvView view;
   int device, sm_count;
   void* encode;              // the driver's cuTensorMapEncodeTiled
-  CUtensorMap map_k, map_v;  // the codes in boxes of 16 tokens by at most 128 bytes, swizzled
+  // The codes as rows of bytes, in boxes of at most 128 bytes by as many tokens as a unit of the
+  // kernel and a page both hold: few-rows kernel, and (fp16) many-rows kernel.
+  CUtensorMap map_k, map_v, wide_k, wide_v;
 };
+
+namespace qtea {
+// log2 of the tokens of a unit of the few-rows kernel: 8 KB of keys and values at head_dim 128.
+__host__ __device__ constexpr int kv_unit_shift(int format) {
+  return format == QTEA_KV_F16 ? 4 : format == QTEA_KV_FP8 ? 5 : 6;
+}
+}  // namespace qtea

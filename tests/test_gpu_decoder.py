@@ -227,12 +227,15 @@ def test_attention_lengths_and_pages_out_of_range_are_bounded(qt):
     reads nothing outside the cache (addresses are clamped in the kernel) and others' rows stay right."""
     c = Case(qt, "f16", [1, 1, 1], [64, 64, 64], 8, 2, 128, 16, seed=5)
     q = torch.randn(3, 8, 128, device="cuda").half()
-    ref = qt.qtea_attention(c.cache, c.batch, q)
     table = c.batch.pages.clone()
     table[0] = torch.tensor([1 << 30, -(1 << 30), 2, c.cache.n_pages], dtype=torch.int32, device="cuda")
     ctx = torch.tensor([1 << 30, -5, 64], dtype=torch.int32, device="cuda")
     out = qt.qtea_attention(c.cache, qt.KVBatch(c.batch.q_start, ctx, table, 3, 1), q)
-    assert torch.equal(out[2], ref[2]) and not out[1].any()
+    assert not out[1].any()
+    # the others' lengths change how the work is split, so the third row is held to its own bound
+    ref, _, spread = od.attention(q[2:].cpu().numpy(), c.seq["k"][2:], c.seq["v"][2:], [1], [64], 128 ** -0.5)
+    err = np.abs(out[2:].cpu().numpy().astype(np.float64) - ref)
+    assert np.all(err <= (2.0 ** -11 + 2.0 ** -12) * spread + 2.0 ** -11 * np.abs(ref) + 2.0 ** -16)
 
 
 def test_attention_replays_in_a_graph_with_other_lengths(qt):
