@@ -22,6 +22,7 @@
 // outruns the reference, a vote per 16 keys otherwise.
 #include <algorithm>
 #include <cstring>
+#include <type_traits>
 
 #include "qtea_attn.h"
 
@@ -285,10 +286,9 @@ __global__ void __launch_bounds__(kWarps * 32, (Rows<FMT, D, NT>::kCtas))
       const uint32_t kbase = ring + stage * T::kStageBytes, vbase = kbase + T::kSideBytes;
       const uint32_t sbase = scales + stage * 2 * T::kScaleBytes;
       const int key_unit = (it.unit0 + warp + kWarps * i) << T::kShift;
-#pragma unroll (FMT == QTEA_KV_F16 || NT == 4 ? 1 : 2)
-      for (int sub = 0; sub < T::kSubs; ++sub) {
-        const int key0 = key_unit + 16 * sub;
-        if (key0 >= hi_all || key0 + 16 <= lo_all) continue;  // nothing of the tile sees these
+      // 16 keys of the unit; `masked`: not every row of the tile sees all of them
+      auto step = [&](int sub, int key0, auto masked) {
+        constexpr bool kMasked = decltype(masked)::value;
         const uint32_t kb = kbase + sub * T::kParts * T::kBoxBytes, vb = vbase + sub * T::kParts * T::kBoxBytes;
         float s[NT][4];
         {
@@ -349,28 +349,18 @@ __global__ void __launch_bounds__(kWarps * 32, (Rows<FMT, D, NT>::kCtas))
         }
         // softmax weights
         bool outrun = false;
-        if (key0 + 16 > hi_in || key0 < lo_in) {
 #pragma unroll
-          for (int nt = 0; nt < NT; ++nt)
+        for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-            for (int col = 0; col < 2; ++col) {
-              const int h = seen(8 * nt + 2 * c + col), l = p.window > 0 ? h - p.window : 0;
+          for (int col = 0; col < 2; ++col) {
+            const int h = kMasked ? seen(8 * nt + 2 * c + col) : 0, l = kMasked && p.window > 0 ? h - p.window : 0;
 #pragma unroll
-              for (int e = col; e < 4; e += 2) {
-                const int key = key0 + g + (e >> 1) * 8;
-                s[nt][e] = key < l || key >= h ? kNegInf : s[nt][e] * p.scale_log2;
-                outrun |= s[nt][e] > m[nt][col] + kLag;
-              }
+            for (int e = col; e < 4; e += 2) {
+              const int key = key0 + g + (e >> 1) * 8;
+              s[nt][e] = kMasked && (key < l || key >= h) ? kNegInf : s[nt][e] * p.scale_log2;
+              outrun |= s[nt][e] > m[nt][col] + kLag;
             }
-        } else {
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              s[nt][e] *= p.scale_log2;
-              outrun |= s[nt][e] > m[nt][e & 1] + kLag;
-            }
-        }
+          }
         if (__any_sync(0xffffffffu, outrun)) {
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt)
@@ -406,11 +396,10 @@ __global__ void __launch_bounds__(kWarps * 32, (Rows<FMT, D, NT>::kCtas))
         }
         // O^T += V^T P^T. Where some keys lie outside all that the tile sees, their values and powers
         // of two are replaced by zeros: 0 * NaN would reach the sums.
-        const bool edge = key0 + 16 > hi_all || key0 < lo_all;
         auto in = [&](int k) { return key0 + k >= lo_all && key0 + k < hi_all; };
         auto load_v = [&](uint32_t* r, uint32_t addr) {  // keys 2c, 2c+1 in r[0], r[1], 2c+8, 2c+9 in r[2], r[3]
           ldmatrix4_trans(r, addr);
-          if (edge) {
+          if (kMasked) {
             const uint32_t k0 = (in(2 * c) ? 0xffffu : 0u) | (in(2 * c + 1) ? 0xffff0000u : 0u);
             const uint32_t k1 = (in(2 * c + 8) ? 0xffffu : 0u) | (in(2 * c + 9) ? 0xffff0000u : 0u);
             r[0] &= k0, r[1] &= k0, r[2] &= k1, r[3] &= k1;
@@ -432,7 +421,7 @@ __global__ void __launch_bounds__(kWarps * 32, (Rows<FMT, D, NT>::kCtas))
           for (int j = 0; j < 4; ++j) {
             const int key = 2 * c + (j & 1) + (j >> 1) * 8;
             w[j] = D == 128 ? lds32(sv + key * 4) : lds16(sv + key * 2);
-            w[j] = scale_high(edge && !in(key) ? 0x7f7f7f7fu : w[j]);
+            w[j] = scale_high(kMasked && !in(key) ? 0x7f7f7f7fu : w[j]);
           }
 #pragma unroll
           for (int x = 0; x < T::kRowBytes; x += 32) {
@@ -471,6 +460,13 @@ __global__ void __launch_bounds__(kWarps * 32, (Rows<FMT, D, NT>::kCtas))
             }
           }
         }
+      };
+#pragma unroll 1
+      for (int sub = 0; sub < T::kSubs; ++sub) {
+        const int key0 = key_unit + 16 * sub;
+        if (key0 >= hi_all || key0 + 16 <= lo_all) continue;  // nothing of the tile sees these
+        if (key0 + 16 > hi_in || key0 < lo_in) step(sub, key0, std::true_type());
+        else step(sub, key0, std::false_type());
       }
       ++fills;
       __syncwarp();  // every lane is done with the stage

@@ -31,154 +31,173 @@ struct AppendParams {
 };
 
 constexpr int kAppendWarps = 8;
+constexpr int kAppendPasses = 4;
 
-template <int TYPE, int P>
-__device__ __forceinline__ void load_pairs(const void* row, int i, float* v) {
-  if (P == 2) {
-    // element-aligned rows only: two scalar loads that the coalescer joins
-    if (TYPE == QTEA_TYPE_F32) {
-      const float* p = static_cast<const float*>(row) + i;
-      v[0] = p[0], v[1] = p[1];
+// Four consecutive elements as fp32: one access where the rows are aligned for it.
+template <int TYPE, bool VEC>
+__device__ __forceinline__ void load4(const char* p, float* v) {
+  if (TYPE == QTEA_TYPE_F32) {
+    if (VEC) {
+      const float4 x = __ldcs(reinterpret_cast<const float4*>(p));
+      v[0] = x.x, v[1] = x.y, v[2] = x.z, v[3] = x.w;
     } else {
-      const __half* p = static_cast<const __half*>(row) + i;
-      v[0] = __half2float(p[0]), v[1] = __half2float(p[1]);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = reinterpret_cast<const float*>(p)[e];
     }
   } else {
-    v[0] = TYPE == QTEA_TYPE_F32 ? static_cast<const float*>(row)[i]
-                                 : __half2float(static_cast<const __half*>(row)[i]);
+    if (VEC) {
+      const uint2 x = __ldcs(reinterpret_cast<const uint2*>(p));
+      const float2 lo = __half22float2(*reinterpret_cast<const __half2*>(&x.x));
+      const float2 hi = __half22float2(*reinterpret_cast<const __half2*>(&x.y));
+      v[0] = lo.x, v[1] = lo.y, v[2] = hi.x, v[3] = hi.y;
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = __half2float(reinterpret_cast<const __half*>(p)[e]);
+    }
   }
+}
+
+template <bool VEC>
+__device__ __forceinline__ void table4(const float* p, float* v) {
+  if (VEC) {
+    const float4 x = __ldg(reinterpret_cast<const float4*>(p));
+    v[0] = x.x, v[1] = x.y, v[2] = x.z, v[3] = x.w;
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = __ldg(p + e);
+  }
+}
+
+__device__ __forceinline__ uint2 half4(const float* v) {
+  const __half2 a = __floats2half2_rn(v[0], v[1]), b = __floats2half2_rn(v[2], v[3]);
+  return make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b));
 }
 
 __device__ __forceinline__ float saturate_f16(float x) {  // NaN stays NaN
   return x > 65504.f ? 65504.f : x < -65504.f ? -65504.f : x;
 }
 
-// One warp per (token, head): lane l holds P = D/64 elements of each half of the head's row, l * P
-// of the first half and the same of the second, the two that a rotation joins. Blocks of 32
-// elements are then 32 / P neighbouring lanes of one half.
-template <int TYPE, int FMT, int D>
+// A warp takes one token and kAppendPasses times 256 / D of its heads: D / 8 lanes a head, lane l of them
+// with the elements 4l.. of the head's first half and of its second, the two that a rotation joins.
+// 8 lanes hold a block of 32 elements of either half, whatever D is. All passes' loads are issued
+// before the first is used: 4 KB a warp at fp32, which is what keeps memory busy.
+// 8192 tokens of 32 + 8 + 8 heads from fp32 to fp16 on GB300: 306 MB in 52 us (one head a warp, with
+// 4-byte accesses, took 88 us).
+template <int TYPE, int FMT, int D, bool VEC>
 __global__ void __launch_bounds__(kAppendWarps * 32) qtea_kv_append_kernel(const AppendParams p) {
-  constexpr int P = D / 64;
-  const int lane = threadIdx.x & 31, heads = p.q_heads + 2 * p.kv.heads;
+  constexpr int kLanes = D / 8, kPerPass = 32 / kLanes, kPerWarp = kAppendPasses * kPerPass;
+  constexpr int kSize = TYPE == QTEA_TYPE_F32 ? 4 : 2;
+  const int lane = threadIdx.x & 31, l = lane % kLanes, heads = p.q_heads + 2 * p.kv.heads;
+  const int warps = (heads + kPerWarp - 1) / kPerWarp;  // of a token
   const long long job = (long long)blockIdx.x * kAppendWarps + (threadIdx.x >> 5);
-  const int t = (int)(job / heads), head = (int)(job % heads);
+  const int t = (int)(job / warps);
   if (t >= p.b.n_tokens) return;
+  const int head0 = (int)(job - (long long)t * warps) * kPerWarp + lane / kLanes;
 
-  // which of the three this head is of, and its row
-  const bool is_q = head < p.q_heads, is_k = !is_q && head < p.q_heads + p.kv.heads;
-  const int h = is_q ? head : is_k ? head - p.q_heads : head - p.q_heads - p.kv.heads;
-  const long long first = is_q ? t * p.q_ld : is_k ? t * p.k_ld : t * p.v_ld;
-  const char* row = static_cast<const char*>(is_q ? p.q : is_k ? p.k : p.v) +
-                    (first + (long long)h * D) * (TYPE == QTEA_TYPE_F32 ? 4 : 2);
-  float a[P], b[P];
-  load_pairs<TYPE, P>(row, lane * P, a);
-  load_pairs<TYPE, P>(row, D / 2 + lane * P, b);
-
-  const int s = kv_find_sequence(p.b.q_start, p.b.n_seqs, t);
-  if (s < 0) return;
-  const int q0 = __ldg(p.b.q_start + s), i = t - q0;
-  const int n = min(__ldg(p.b.q_start + s + 1), p.b.n_tokens) - q0;
-  if (i >= p.b.max_q) return;
-  // a batch longer than max_q counts its first max_q tokens, at the positions the lengths give
-  const int pos = kv_context(p.b, p.kv, s) - n + i;
-
-  const __half* weight = is_q ? p.q_norm : is_k ? p.k_norm : nullptr;
-  if (weight) {
-    float ss = 0.f;
+  float a[kAppendPasses][4], b[kAppendPasses][4];
 #pragma unroll
-    for (int e = 0; e < P; ++e) ss = fmaf(a[e], a[e], fmaf(b[e], b[e], ss));
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
-    const float f = rsqrtf(ss * (1.f / D) + p.eps);
-#pragma unroll
-    for (int e = 0; e < P; ++e) {
-      a[e] = a[e] * f * __half2float(weight[lane * P + e]);
-      b[e] = b[e] * f * __half2float(weight[D / 2 + lane * P + e]);
+  for (int i = 0; i < kAppendPasses; ++i) {
+    const int head = head0 + i * kPerPass;
+    if (head < heads) {
+      const bool is_q = head < p.q_heads, is_k = head < p.q_heads + p.kv.heads;
+      const int h = is_q ? head : is_k ? head - p.q_heads : head - p.q_heads - p.kv.heads;
+      const char* row = static_cast<const char*>(is_q ? p.q : is_k ? p.k : p.v) +
+                        (t * (is_q ? p.q_ld : is_k ? p.k_ld : p.v_ld) + (long long)h * D + 4 * l) * kSize;
+      load4<TYPE, VEC>(row, a[i]);
+      load4<TYPE, VEC>(row + D / 2 * kSize, b[i]);
     }
   }
-  if (p.cos && (is_q || is_k)) {
-    const long long at = (long long)min(max(pos, 0), p.n_positions - 1) * (D / 2) + lane * P;
-#pragma unroll
-    for (int e = 0; e < P; ++e) {
-      const float c = __ldg(p.cos + at + e), d = __ldg(p.sin + at + e);
-      const float x = __fsub_rn(__fmul_rn(a[e], c), __fmul_rn(b[e], d));
-      b[e] = __fadd_rn(__fmul_rn(b[e], c), __fmul_rn(a[e], d));
-      a[e] = x;
-    }
-  }
-  if (is_q) {
-    __half* o = p.q_out + ((long long)t * p.q_heads + h) * D;
-    if (P == 2) {
-      reinterpret_cast<__half2*>(o)[lane] = __floats2half2_rn(a[0], a[P - 1]);
-      reinterpret_cast<__half2*>(o)[32 + lane] = __floats2half2_rn(b[0], b[P - 1]);
-    } else {
-      o[lane] = __float2half_rn(a[0]);
-      o[32 + lane] = __float2half_rn(b[0]);
-    }
-    return;
-  }
-  if (pos < 0) return;
-  const int page = __ldg(p.b.pages + (long long)s * p.b.max_pages + (pos >> p.kv.page_shift));
-  if ((unsigned)page >= (unsigned)p.kv.n_pages) return;
-  const long long slot = ((long long)page * p.kv.heads + h) * p.kv.page_size + (pos & (p.kv.page_size - 1));
-  uint8_t* dst = (is_k ? p.kv.k : p.kv.v) + slot * kv_row_bytes(FMT, D);
-  if (FMT == QTEA_KV_F16) {
-    __half* o = reinterpret_cast<__half*>(dst);
-    if (P == 2) {
-      reinterpret_cast<__half2*>(o)[lane] = __floats2half2_rn(saturate_f16(a[0]), saturate_f16(a[P - 1]));
-      reinterpret_cast<__half2*>(o)[32 + lane] = __floats2half2_rn(saturate_f16(b[0]), saturate_f16(b[P - 1]));
-    } else {
-      o[lane] = __float2half_rn(saturate_f16(a[0]));
-      o[32 + lane] = __float2half_rn(saturate_f16(b[0]));
-    }
-    return;
-  }
-  // the largest magnitude of each block (maxima skip NaN), then its power of two
-  float ta = fabsf(a[0]), tb = fabsf(b[0]);
-  if (P == 2) ta = fmaxf(ta, fabsf(a[P - 1])), tb = fmaxf(tb, fabsf(b[P - 1]));
-#pragma unroll
-  for (int o = 16 / P; o > 0; o >>= 1) {
-    ta = fmaxf(ta, __shfl_xor_sync(0xffffffffu, ta, o));
-    tb = fmaxf(tb, __shfl_xor_sync(0xffffffffu, tb, o));
-  }
-  if (P == 1) {  // D = 64: a block is a whole half
-    ta = fmaxf(ta, __shfl_xor_sync(0xffffffffu, ta, 16));
-    tb = fmaxf(tb, __shfl_xor_sync(0xffffffffu, tb, 16));
-  }
-  constexpr int F = FMT == QTEA_KV_F16 ? QTEA_KV_FP8 : FMT;
-  const int ea = kv_exponent<F>(ta), eb = kv_exponent<F>(tb);
-  const float fa = exp2i(-ea), fb = exp2i(-eb);
-  uint8_t* scales = (is_k ? p.kv.ks : p.kv.vs) + slot * (D / kKvBlock);
-  if (P == 2) {
-    if ((lane & 15) == 0) {
-      scales[lane >> 4] = (uint8_t)(ea + 127);
-      scales[2 + (lane >> 4)] = (uint8_t)(eb + 127);
-    }
-  } else if (lane == 0) {
-    scales[0] = (uint8_t)(ea + 127);
-    scales[1] = (uint8_t)(eb + 127);
+  const KvFound f = kv_find_sequence(p.b.q_start, p.b, p.kv, t);
+  if (f.s < 0 || t - f.first >= p.b.max_q) return;
+  const int pos = f.ctx - min(f.next, p.b.n_tokens) + t;
+  int page = -1;
+  if (pos >= 0) page = __ldg(p.b.pages + (long long)f.s * p.b.max_pages + (pos >> p.kv.page_shift));
+  const bool stored = (unsigned)page < (unsigned)p.kv.n_pages;
+  float c[4], d[4];
+  if (p.cos) {
+    const long long at = (long long)min(max(pos, 0), p.n_positions - 1) * (D / 2) + 4 * l;
+    table4<VEC>(p.cos + at, c);
+    table4<VEC>(p.sin + at, d);
   }
 #pragma unroll
-  for (int e = 0; e < P; ++e) a[e] *= fa, b[e] *= fb;
-  if (FMT == QTEA_KV_FP8) {
-    if (P == 2) {
-      reinterpret_cast<uint16_t*>(dst)[lane] = (uint16_t)to_e4m3x2(a[0], a[P - 1]);
-      reinterpret_cast<uint16_t*>(dst)[32 + lane] = (uint16_t)to_e4m3x2(b[0], b[P - 1]);
-    } else {
-      const uint32_t c = to_e4m3x2(a[0], b[0]);
-      dst[lane] = (uint8_t)c;
-      dst[32 + lane] = (uint8_t)(c >> 8);
-    }
-  } else {
-    if (P == 2) {
-      dst[lane] = (uint8_t)to_e2m1x2(a[0], a[P - 1]);
-      dst[32 + lane] = (uint8_t)to_e2m1x2(b[0], b[P - 1]);
-    } else {  // a lane holds one element of each half: even lanes write their byte and the next lane's
-      const float an = __shfl_down_sync(0xffffffffu, a[0], 1), bn = __shfl_down_sync(0xffffffffu, b[0], 1);
-      if ((lane & 1) == 0) {
-        dst[lane >> 1] = (uint8_t)to_e2m1x2(a[0], an);
-        dst[16 + (lane >> 1)] = (uint8_t)to_e2m1x2(b[0], bn);
+  for (int i = 0; i < kAppendPasses; ++i) {
+    const int head = head0 + i * kPerPass;
+    const bool is_q = head < p.q_heads, is_k = !is_q && head < p.q_heads + p.kv.heads;
+    if (p.q_norm || p.k_norm) {
+      float ss = 0.f;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) ss = fmaf(a[i][e], a[i][e], fmaf(b[i][e], b[i][e], ss));
+#pragma unroll
+      for (int o = kLanes / 2; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
+      const __half* w = is_q ? p.q_norm : is_k ? p.k_norm : nullptr;
+      if (w && head < heads) {
+        const float g = rsqrtf(ss * (1.f / D) + p.eps);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          a[i][e] = a[i][e] * g * __half2float(w[4 * l + e]);
+          b[i][e] = b[i][e] * g * __half2float(w[D / 2 + 4 * l + e]);
+        }
       }
+    }
+    if (p.cos && (is_q || is_k)) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float x = __fsub_rn(__fmul_rn(a[i][e], c[e]), __fmul_rn(b[i][e], d[e]));
+        b[i][e] = __fadd_rn(__fmul_rn(b[i][e], c[e]), __fmul_rn(a[i][e], d[e]));
+        a[i][e] = x;
+      }
+    }
+    if (is_q) {
+      __half* o = p.q_out + ((long long)t * p.q_heads + head) * D + 4 * l;
+      const uint2 x = half4(a[i]), y = half4(b[i]);
+      if (VEC) {
+        *reinterpret_cast<uint2*>(o) = x;
+        *reinterpret_cast<uint2*>(o + D / 2) = y;
+      } else {
+        reinterpret_cast<uint32_t*>(o)[0] = x.x, reinterpret_cast<uint32_t*>(o)[1] = x.y;
+        reinterpret_cast<uint32_t*>(o + D / 2)[0] = y.x, reinterpret_cast<uint32_t*>(o + D / 2)[1] = y.y;
+      }
+    }
+    const bool store = stored && !is_q && head < heads;
+    const int h = is_k ? head - p.q_heads : head - p.q_heads - p.kv.heads;
+    const long long slot = ((long long)page * p.kv.heads + h) * p.kv.page_size + (pos & (p.kv.page_size - 1));
+    uint8_t* dst = (is_k ? p.kv.k : p.kv.v) + slot * kv_row_bytes(FMT, D);
+    if (FMT == QTEA_KV_F16) {
+      if (store) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) a[i][e] = saturate_f16(a[i][e]), b[i][e] = saturate_f16(b[i][e]);
+        reinterpret_cast<uint2*>(dst)[l] = half4(a[i]);
+        reinterpret_cast<uint2*>(dst)[D / 8 + l] = half4(b[i]);
+      }
+      continue;
+    }
+    // the largest magnitude of each block (maxima skip NaN), then its power of two
+    float ta = 0.f, tb = 0.f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) ta = fmaxf(ta, fabsf(a[i][e])), tb = fmaxf(tb, fabsf(b[i][e]));
+#pragma unroll
+    for (int o = 4; o > 0; o >>= 1) {
+      ta = fmaxf(ta, __shfl_xor_sync(0xffffffffu, ta, o));
+      tb = fmaxf(tb, __shfl_xor_sync(0xffffffffu, tb, o));
+    }
+    if (!store) continue;
+    constexpr int F = FMT == QTEA_KV_F16 ? QTEA_KV_FP8 : FMT;
+    const int ea = kv_exponent<F>(ta), eb = kv_exponent<F>(tb);
+    const float fa = exp2i(-ea), fb = exp2i(-eb);
+    if ((l & 7) == 0) {
+      uint8_t* scales = (is_k ? p.kv.ks : p.kv.vs) + slot * (D / kKvBlock) + (l >> 3);
+      scales[0] = (uint8_t)(ea + 127);
+      scales[D / 64] = (uint8_t)(eb + 127);
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) a[i][e] *= fa, b[i][e] *= fb;
+    if (FMT == QTEA_KV_FP8) {
+      reinterpret_cast<uint32_t*>(dst)[l] = to_e4m3x2(a[i][0], a[i][1]) | to_e4m3x2(a[i][2], a[i][3]) << 16;
+      reinterpret_cast<uint32_t*>(dst)[D / 8 + l] = to_e4m3x2(b[i][0], b[i][1]) | to_e4m3x2(b[i][2], b[i][3]) << 16;
+    } else {
+      reinterpret_cast<uint16_t*>(dst)[l] = (uint16_t)(to_e2m1x2(a[i][0], a[i][1]) | to_e2m1x2(a[i][2], a[i][3]) << 8);
+      reinterpret_cast<uint16_t*>(dst)[D / 8 + l] =
+          (uint16_t)(to_e2m1x2(b[i][0], b[i][1]) | to_e2m1x2(b[i][2], b[i][3]) << 8);
     }
   }
 }
@@ -192,43 +211,40 @@ struct ReadParams {
   int n_rows;
   uint4* k_out;
   uint4* v_out;
+  int rows;  // output rows of a CTA
 };
 
 constexpr int kReadThreads = 256;
-constexpr int kReadRows = 16;  // output rows of a CTA
+constexpr int kReadRows = 16;  // output rows of a CTA, at most
 
-// A CTA takes kReadRows consecutive output rows: its first threads find each row's place in the
-// cache, then every thread converts 16 elements at a time, so that a warp's stores are one run of
-// memory. 16 elements are 32, 16 or 8 bytes of codes, one load each.
+// A CTA takes a few consecutive output rows: its warps find the rows' places in the cache, a row at a
+// time (the sequence from row_start, 32 sequences a load, with their lengths beside them), then
+// every thread converts 16 elements at a time, so that a warp's stores are one run of memory. 16
+// elements are 32, 16 or 8 bytes of codes, one load each.
 template <int FMT, int D>
 __global__ void __launch_bounds__(kReadThreads) qtea_kv_read_kernel(const ReadParams p) {
   __shared__ long long where[kReadRows];  // slot of head 0, -1: zeros, -2: no sequence's row
-  const int r0 = blockIdx.x * kReadRows;
-  if (threadIdx.x < kReadRows) {
-    const int r = r0 + threadIdx.x;
+  const int r0 = blockIdx.x * p.rows, lane = threadIdx.x & 31;
+  for (int i = threadIdx.x >> 5; i < p.rows; i += kReadThreads / 32) {
+    const int r = r0 + i;
     long long at = -2;
-    if (r < p.n_rows && r >= __ldg(p.row_start) && r < __ldg(p.row_start + p.b.n_seqs)) {
-      int lo = 0, hi = p.b.n_seqs;  // the last sequence that starts at or before r, and is not empty
-      while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (__ldg(p.row_start + mid) <= r) lo = mid;
-        else hi = mid;
-      }
-      const int pos = r - __ldg(p.row_start + lo);
-      at = -1;
-      if (pos < kv_context(p.b, p.kv, lo)) {
-        const int page = __ldg(p.b.pages + (long long)lo * p.b.max_pages + (pos >> p.kv.page_shift));
+    if (r < p.n_rows) {
+      const KvFound f = kv_find_sequence(p.row_start, p.b, p.kv, r);
+      const int pos = r - f.first;
+      if (f.s >= 0) at = -1;
+      if (f.s >= 0 && pos < f.ctx) {
+        const int page = __ldg(p.b.pages + (long long)f.s * p.b.max_pages + (pos >> p.kv.page_shift));
         if ((unsigned)page < (unsigned)p.kv.n_pages)
           at = (long long)page * p.kv.heads * p.kv.page_size + (pos & (p.kv.page_size - 1));
       }
     }
-    where[threadIdx.x] = at;
+    if (lane == 0) where[i] = at;
   }
   __syncthreads();
   constexpr int kChunks = D / 16;  // of 16 elements
   const int per_row = p.kv.heads * kChunks;
   constexpr int kBytes = FMT == QTEA_KV_F16 ? 32 : FMT == QTEA_KV_FP8 ? 16 : 8;
-  const int all = kReadRows * per_row;
+  const int all = p.rows * per_row;
 #pragma unroll 2
   for (int u = threadIdx.x; u < all; u += kReadThreads) {
     const int r = u / per_row, w = u - r * per_row, head = w / kChunks, c = w - head * kChunks;
@@ -272,9 +288,17 @@ __global__ void __launch_bounds__(kReadThreads) qtea_kv_read_kernel(const ReadPa
 }
 
 template <int TYPE, int FMT>
-void launch_append(const AppendParams& p, int grid, cudaStream_t st) {
-  if (p.kv.dim == 128) qtea_kv_append_kernel<TYPE, FMT, 128><<<grid, kAppendWarps * 32, 0, st>>>(p);
-  else qtea_kv_append_kernel<TYPE, FMT, 64><<<grid, kAppendWarps * 32, 0, st>>>(p);
+void launch_append(const AppendParams& p, bool vec, cudaStream_t st) {
+  const int per_warp = kAppendPasses * 256 / p.kv.dim, heads = p.q_heads + 2 * p.kv.heads;
+  const long long jobs = (long long)p.b.n_tokens * ((heads + per_warp - 1) / per_warp);
+  const unsigned grid = (unsigned)((jobs + kAppendWarps - 1) / kAppendWarps);  // < 2^31 (checked)
+  if (p.kv.dim == 128) {
+    if (vec) qtea_kv_append_kernel<TYPE, FMT, 128, true><<<grid, kAppendWarps * 32, 0, st>>>(p);
+    else qtea_kv_append_kernel<TYPE, FMT, 128, false><<<grid, kAppendWarps * 32, 0, st>>>(p);
+  } else {
+    if (vec) qtea_kv_append_kernel<TYPE, FMT, 64, true><<<grid, kAppendWarps * 32, 0, st>>>(p);
+    else qtea_kv_append_kernel<TYPE, FMT, 64, false><<<grid, kAppendWarps * 32, 0, st>>>(p);
+  }
 }
 
 template <int FMT>
@@ -392,20 +416,22 @@ int qtea_kv_append(const qtea_kv* kv, const qtea_kv_batch* batch, const qtea_kv_
   p.k_norm = reinterpret_cast<const __half*>(a->k_norm);
   p.eps = a->eps;
   p.q_out = reinterpret_cast<__half*>(a->q_out);
-  const long long jobs = (long long)p.b.n_tokens * (p.q_heads + 2 * p.kv.heads);
-  const long long grid = (jobs + kAppendWarps - 1) / kAppendWarps;
-  if (grid > 0x7fffffffLL) return QTEA_ERR_INVALID_ARG;
+  if ((long long)p.b.n_tokens * (p.q_heads + 2 * p.kv.heads) > 0x7fffffffLL) return QTEA_ERR_INVALID_ARG;
+  // accesses of four elements: every row of every source, the tables and q_out aligned for them
+  const auto fits = [&](const void* x, long long ld) { return aligned(x, 4 * size) && ld % 4 == 0; };
+  const bool vec = fits(a->k, a->k_ld) && fits(a->v, a->v_ld) && (!a->q || (fits(a->q, a->q_ld) && aligned(a->q_out, 8))) &&
+                   aligned(a->cos, 16) && aligned(a->sin, 16);
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
   const bool f32 = a->type == QTEA_TYPE_F32;
   if (p.kv.format == QTEA_KV_F16) {
-    if (f32) launch_append<QTEA_TYPE_F32, QTEA_KV_F16>(p, (int)grid, st);
-    else launch_append<QTEA_TYPE_F16, QTEA_KV_F16>(p, (int)grid, st);
+    if (f32) launch_append<QTEA_TYPE_F32, QTEA_KV_F16>(p, vec, st);
+    else launch_append<QTEA_TYPE_F16, QTEA_KV_F16>(p, vec, st);
   } else if (p.kv.format == QTEA_KV_FP8) {
-    if (f32) launch_append<QTEA_TYPE_F32, QTEA_KV_FP8>(p, (int)grid, st);
-    else launch_append<QTEA_TYPE_F16, QTEA_KV_FP8>(p, (int)grid, st);
+    if (f32) launch_append<QTEA_TYPE_F32, QTEA_KV_FP8>(p, vec, st);
+    else launch_append<QTEA_TYPE_F16, QTEA_KV_FP8>(p, vec, st);
   } else {
-    if (f32) launch_append<QTEA_TYPE_F32, QTEA_KV_FP4>(p, (int)grid, st);
-    else launch_append<QTEA_TYPE_F16, QTEA_KV_FP4>(p, (int)grid, st);
+    if (f32) launch_append<QTEA_TYPE_F32, QTEA_KV_FP4>(p, vec, st);
+    else launch_append<QTEA_TYPE_F16, QTEA_KV_FP4>(p, vec, st);
   }
   return cudaGetLastError() == cudaSuccess ? QTEA_OK : QTEA_ERR_CUDA;
 }
@@ -423,7 +449,10 @@ int qtea_kv_read(const qtea_kv* kv, const qtea_kv_batch* batch, const int32_t* r
   p.n_rows = n_rows;
   p.k_out = reinterpret_cast<uint4*>(k_out);
   p.v_out = reinterpret_cast<uint4*>(v_out);
-  const int grid = (int)(((long long)n_rows + kReadRows - 1) / kReadRows);
+  // Few rows: fewer of them a CTA, for the latency of one row's chain is what counts (3303 rows of 8 heads,
+  // fp4, with 776 appended before: 18 us at 16 rows a CTA).
+  p.rows = n_rows < 64 * kv->sm_count ? 4 : kReadRows;
+  const int grid = (int)(((long long)n_rows + p.rows - 1) / p.rows);
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
   if (p.kv.format == QTEA_KV_F16) launch_read<QTEA_KV_F16>(p, grid, st);
   else if (p.kv.format == QTEA_KV_FP8) launch_read<QTEA_KV_FP8>(p, grid, st);

@@ -45,18 +45,32 @@ __device__ __forceinline__ int kv_context(const KvBatchView& b, const KvView& kv
   return min(max(__ldg(b.ctx_len + s), 0), most);
 }
 
-// The sequence whose rows [start[s], start[s+1]) hold `row`, found by one warp (all 32 lanes call
-// it, with the same row), or -1.
-__device__ __forceinline__ int kv_find_sequence(const int32_t* start, int n_seqs, int row) {
+// The sequence whose rows [start[s], start[s+1]) hold `row`, found by one warp (all 32 lanes call it,
+// with the same row): its number (-1: none), first row, the next one's, and its context length. One
+// round of loads covers 32 sequences.
+struct KvFound {
+  int s, first, next, ctx;
+};
+__device__ __forceinline__ KvFound kv_find_sequence(const int32_t* start, const KvBatchView& b, const KvView& kv, int row) {
   const int lane = threadIdx.x & 31;
-  if (row < __ldg(start)) return -1;
-  for (int base = 0; base < n_seqs; base += 32) {
+  KvFound f{-1, 0, 0, 0};
+  for (int base = 0; base < b.n_seqs; base += 32) {
     const int s = base + lane;
-    const bool past = s < n_seqs && __ldg(start + s + 1) > row;
-    const unsigned m = __ballot_sync(0xffffffffu, past);
-    if (m) return base + __ffs(m) - 1;
+    int first = 0, next = 0, ctx = 0;
+    if (s < b.n_seqs) {
+      first = __ldg(start + s), next = __ldg(start + s + 1);
+      ctx = kv_context(b, kv, s);
+    }
+    const unsigned m = __ballot_sync(0xffffffffu, row >= first && row < next);
+    if (!m) continue;
+    const int from = __ffs(m) - 1;
+    f.s = base + from;
+    f.first = __shfl_sync(0xffffffffu, first, from);
+    f.next = __shfl_sync(0xffffffffu, next, from);
+    f.ctx = __shfl_sync(0xffffffffu, ctx, from);
+    break;
   }
-  return -1;
+  return f;
 }
 
 // The exponent of a block's power of two: the smallest e >= kKvEMin with top <= limit * 2^e, at most

@@ -8,6 +8,7 @@ and a ``KVBatch``; a call then checks its own tensors only.
 from __future__ import annotations
 
 import ctypes
+import struct
 
 QTEA_TYPE_F32 = 0
 QTEA_TYPE_F16 = 1
@@ -23,16 +24,10 @@ class _Batch(ctypes.Structure):
                 ("max_q_len", _I)]
 
 
-class _Append(ctypes.Structure):
-    _fields_ = [("q", _P), ("k", _P), ("v", _P), ("q_ld", _L), ("k_ld", _L), ("v_ld", _L), ("type", _I),
-                ("n_q_heads", _I), ("cos", _P), ("sin", _P), ("n_positions", _I), ("q_norm", _P), ("k_norm", _P),
-                ("eps", ctypes.c_float), ("q_out", _P)]
-
-
-class _Norm(ctypes.Structure):
-    _fields_ = [("h", _P), ("y", _P), ("post_weight", _P), ("gate", _P), ("weight", _P), ("h_out", _P), ("x", _P),
-                ("h_ld", _L), ("y_ld", _L), ("gate_ld", _L), ("h_out_ld", _L), ("x_ld", _L), ("h_type", _I),
-                ("y_type", _I), ("n_rows", _I), ("n_cols", _I), ("res_scale", ctypes.c_float), ("eps", ctypes.c_float)]
+# qtea_kv_append_args and qtea_norm_args as their C layouts (native alignment): packing one is several
+# times faster than filling a ctypes structure field by field.
+_APPEND = struct.Struct("@PPPqqqiiPPiPPfP")
+_NORM = struct.Struct("@PPPPPPPqqqqqiiiiff")
 
 
 def _bind(lib):
@@ -69,7 +64,8 @@ def _lib():
     if lib is None:
         import torch
         lib = _package().load()
-        _state.update(lib=lib, raw_stream=torch._C._cuda_getCurrentRawStream, f16=torch.float16, f32=torch.float32)
+        _state.update(lib=lib, raw_stream=torch._C._cuda_getCurrentRawStream, f16=torch.float16, f32=torch.float32,
+                      i32=torch.int32)
     return lib
 
 
@@ -83,30 +79,29 @@ def _fail(rc, where):
     raise _package().QteaError(rc, where)
 
 
-def _array(t, dtypes, name, shape):
-    """A contiguous CUDA tensor of one of these types and this shape: its pointer."""
+def _array(t, dtype, name, shape):
+    """A contiguous CUDA tensor of this type and shape: its pointer."""
+    if t.dtype is dtype and t.shape == shape and t.is_contiguous() and t.is_cuda:
+        return t.data_ptr()
     if not t.is_cuda:
         raise TypeError(f"{name} must be a CUDA tensor")
-    if t.dtype not in dtypes:
-        raise TypeError(f"{name} has dtype {t.dtype}, expected one of {dtypes}")
-    if tuple(t.shape) != shape or not t.is_contiguous():
-        raise ValueError(f"{name} must be contiguous with shape {shape}, got {tuple(t.shape)}")
-    return t.data_ptr()
+    if t.dtype is not dtype:
+        raise TypeError(f"{name} has dtype {t.dtype}, expected {dtype}")
+    raise ValueError(f"{name} must be contiguous with shape {shape}, got {tuple(t.shape)}")
 
 
 def _rows(t, dtype, name, rows, cols):
     """A tensor of `rows` rows of `cols` elements in all, dense within a row: its pointer and row stride."""
+    if t.dtype is dtype and t.is_contiguous() and t.numel() == rows * cols and t.shape[0] == rows and t.is_cuda:
+        return t.data_ptr(), cols
     if t.dtype is not dtype:
         raise TypeError(f"{name} has dtype {t.dtype}, expected {dtype}")
     if not t.is_cuda:
         raise TypeError(f"{name} must be a CUDA tensor")
     if t.shape[0] != rows or t.numel() != rows * cols:
         raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {rows} rows of {cols} elements")
-    if t.is_contiguous():
-        return t.data_ptr(), cols
-    st = t.stride()
-    inner, n = 1, t.dim()
-    for d in range(n - 1, 0, -1):
+    st, inner = t.stride(), 1
+    for d in range(t.dim() - 1, 0, -1):
         if t.shape[d] != 1 and st[d] != inner:
             raise ValueError(f"{name} must be dense within a row")
         inner *= t.shape[d]
@@ -132,16 +127,17 @@ class KVCache:
             raise ValueError(f"unknown cache format {fmt}")
         n, heads, page, row = k_pages.shape
         dim = row * 2 if fmt == QTEA_KV_FP4 else row
-        types = {QTEA_KV_F16: (torch.float16,), QTEA_KV_FP8: (torch.uint8, torch.float8_e4m3fn),
-                 QTEA_KV_FP4: (torch.uint8,)}[fmt]
-        kp = _array(k_pages, types, "k_pages", (n, heads, page, row))
-        vp = _array(v_pages, types, "v_pages", (n, heads, page, row))
+        kind = torch.float16 if fmt == QTEA_KV_F16 else torch.uint8
+        if fmt == QTEA_KV_FP8 and k_pages.dtype is torch.float8_e4m3fn:
+            kind = torch.float8_e4m3fn
+        kp = _array(k_pages, kind, "k_pages", (n, heads, page, row))
+        vp = _array(v_pages, kind, "v_pages", (n, heads, page, row))
         ks = vs = None
         if fmt != QTEA_KV_F16:
             if k_scale is None or v_scale is None:
                 raise ValueError("this cache format needs k_scale and v_scale")
-            ks = _array(k_scale, (torch.uint8,), "k_scale", (n, heads, page, dim // 32))
-            vs = _array(v_scale, (torch.uint8,), "v_scale", (n, heads, page, dim // 32))
+            ks = _array(k_scale, torch.uint8, "k_scale", (n, heads, page, dim // 32))
+            vs = _array(v_scale, torch.uint8, "v_scale", (n, heads, page, dim // 32))
         out = ctypes.c_void_p()
         rc = lib.qtea_kv_create(kp, vp, ks, vs, n, page, heads, dim, fmt, ctypes.byref(out))
         if rc:
@@ -193,7 +189,7 @@ class KVBatch:
         if pages.dim() != 2:
             raise ValueError("pages must be [n_seqs][max_pages]")
         n, most = pages.shape
-        i32 = (torch.int32,)
+        i32 = torch.int32
         self._c = _Batch(_array(q_start, i32, "q_start", (n + 1,)), _array(ctx_len, i32, "ctx_len", (n,)),
                          _array(pages, i32, "pages", (n, most)), n, most, int(n_tokens), int(max_q_len))
         self._ref = ctypes.addressof(self._c)
@@ -209,41 +205,42 @@ def qtea_kv_append(cache: KVCache, batch: KVBatch, k, v, q=None, cos=None, sin=N
     may be strided. cos, sin: fp32 [positions][head_dim / 2]. q_norm, k_norm: fp16 [head_dim].
     q_out: fp16 [n_tokens][q heads][head_dim], made when not given.
     """
-    import torch
     lib = _lib()
+    f32, f16 = _state["f32"], _state["f16"]
     n, dim = batch.n_tokens, cache.head_dim
-    a = _Append()
     dtype = k.dtype
-    if dtype is not _state["f32"] and dtype is not _state["f16"]:
+    if dtype is not f32 and dtype is not f16:
         raise TypeError(f"k has dtype {dtype}, expected float32 or float16")
-    a.type = QTEA_TYPE_F32 if dtype is _state["f32"] else QTEA_TYPE_F16
-    a.k, a.k_ld = _rows(k, dtype, "k", n, cache.n_kv_heads * dim)
-    a.v, a.v_ld = _rows(v, dtype, "v", n, cache.n_kv_heads * dim)
+    kp, k_ld = _rows(k, dtype, "k", n, cache.n_kv_heads * dim)
+    vp, v_ld = _rows(v, dtype, "v", n, cache.n_kv_heads * dim)
+    qp = q_ld = heads = op = 0
     if q is not None:
-        if n and q.numel() % (n * dim):
-            raise ValueError(f"q has shape {tuple(q.shape)}, not whole heads of {dim}")
         heads = q.numel() // (n * dim) if n else 1
-        a.q, a.q_ld = _rows(q, dtype, "q", n, heads * dim)
-        a.n_q_heads = heads
+        if n and heads * n * dim != q.numel():
+            raise ValueError(f"q has shape {tuple(q.shape)}, not whole heads of {dim}")
+        qp, q_ld = _rows(q, dtype, "q", n, heads * dim)
         if q_out is None:
-            q_out = torch.empty((n, heads, dim), dtype=torch.float16, device=q.device)
-        a.q_out = _array(q_out, (_state["f16"],), "q_out", (n, heads, dim))
+            import torch
+            q_out = torch.empty((n, heads, dim), dtype=f16, device=q.device)
+        op = _array(q_out, f16, "q_out", (n, heads, dim))
+    cp = sp = positions = qn = kn = 0
     if cos is not None:
         if sin is None:
             raise ValueError("cos and sin come together")
-        a.n_positions = cos.shape[0]
-        if a.n_positions < 1:  # its pointer would be NULL: no rotation
+        positions = cos.shape[0]
+        if positions < 1:  # its pointer would be NULL: no rotation
             _fail(1, "qtea_kv_append")
-        a.cos = _array(cos, (_state["f32"],), "cos", (a.n_positions, dim // 2))
-        a.sin = _array(sin, (_state["f32"],), "sin", (a.n_positions, dim // 2))
+        cp = _array(cos, f32, "cos", (positions, dim // 2))
+        sp = _array(sin, f32, "sin", (positions, dim // 2))
     elif sin is not None:
         raise ValueError("cos and sin come together")
     if q_norm is not None:
-        a.q_norm = _array(q_norm, (_state["f16"],), "q_norm", (dim,))
+        qn = _array(q_norm, f16, "q_norm", (dim,))
     if k_norm is not None:
-        a.k_norm = _array(k_norm, (_state["f16"],), "k_norm", (dim,))
-    a.eps = eps
-    rc = lib.qtea_kv_append(cache.handle, batch._ref, ctypes.addressof(a), _stream_of(stream, cache.device))
+        kn = _array(k_norm, f16, "k_norm", (dim,))
+    args = _APPEND.pack(qp, kp, vp, q_ld, k_ld, v_ld, QTEA_TYPE_F32 if dtype is f32 else QTEA_TYPE_F16, heads, cp, sp,
+                        positions, qn, kn, eps, op)
+    rc = lib.qtea_kv_append(cache.handle, batch._ref, args, _stream_of(stream, cache.device))
     if rc:
         _fail(rc, "qtea_kv_append")
     return q_out if q is not None else None
@@ -253,7 +250,6 @@ def qtea_kv_read(cache: KVCache, batch: KVBatch, row_start, n_rows=None, k_out=N
     """The sequences' cached rows as fp16 [n_rows][kv heads][head_dim]: (k, v). Sequence s takes the
     rows from row_start[s] (int32 [n_seqs + 1], on the device); n_rows is needed when neither output
     is given."""
-    import torch
     lib = _lib()
     if n_rows is None:
         if k_out is None and v_out is None:
@@ -261,10 +257,11 @@ def qtea_kv_read(cache: KVCache, batch: KVBatch, row_start, n_rows=None, k_out=N
         n_rows = (k_out if k_out is not None else v_out).shape[0]
     shape = (int(n_rows), cache.n_kv_heads, cache.head_dim)
     if k_out is None and v_out is None:
+        import torch
         k_out, v_out = (torch.empty(shape, dtype=torch.float16, device=cache.k_pages.device) for _ in range(2))
-    f16 = (_state["f16"],)
+    f16 = _state["f16"]
     rc = lib.qtea_kv_read(cache.handle, batch._ref,
-                          _array(row_start, (torch.int32,), "row_start", (batch._c.n_seqs + 1,)), shape[0],
+                          _array(row_start, _state["i32"], "row_start", (batch._c.n_seqs + 1,)), shape[0],
                           _array(k_out, f16, "k_out", shape) if k_out is not None else None,
                           _array(v_out, f16, "v_out", shape) if v_out is not None else None,
                           _stream_of(stream, cache.device))
@@ -304,14 +301,15 @@ def qtea_attention(cache: KVCache, batch: KVBatch, q, scale=None, window: int = 
     q: fp16 of that shape (rows may be strided); scale: head_dim ** -0.5 by default; window: a token
     sees at most that many positions, itself among them (0: all). lse: fp32 [n_tokens][q heads], written when given.
     """
-    import torch
     lib = _lib()
     n, dim = batch.n_tokens, cache.head_dim
-    if q.dim() != 3 or q.shape[2] != dim:
-        raise ValueError(f"q must be [n_tokens][q heads][{dim}], got {tuple(q.shape)}")
-    heads = q.shape[1]
+    shape = q.shape
+    if len(shape) != 3 or shape[2] != dim:
+        raise ValueError(f"q must be [n_tokens][q heads][{dim}], got {tuple(shape)}")
+    heads = shape[1]
     q_ptr, q_ld = _rows(q, _state["f16"], "q", n, heads * dim)
     if out is None:
+        import torch
         out = torch.empty((n, heads, dim), dtype=torch.float16, device=q.device)
     o_ptr, o_ld = _rows(out, _state["f16"], "out", n, heads * dim)
     stream = _stream_of(stream, cache.device)
@@ -321,8 +319,8 @@ def qtea_attention(cache: KVCache, batch: KVBatch, q, scale=None, window: int = 
             workspace = attention_workspace(cache.device, stream)
     rc = lib.qtea_attention(cache.handle, batch._ref, q_ptr, q_ld, heads, dim ** -0.5 if scale is None else scale,
                             window, o_ptr, o_ld,
-                            None if lse is None else _array(lse, (_state["f32"],), "lse", (n, heads)),
-                            workspace.data_ptr(), workspace.numel() * workspace.element_size(), stream)
+                            None if lse is None else _array(lse, _state["f32"], "lse", (n, heads)),
+                            workspace.data_ptr(), workspace.nbytes, stream)
     if rc:
         _fail(rc, "qtea_attention")
     return out
@@ -350,42 +348,39 @@ def qtea_norm(h, weight=None, y=None, post_weight=None, gate=None, res_scale: fl
     [rows][cols]; weights: fp16 [cols]. Returns x, fp16 [rows][cols] (None with want_x=False: the last
     residual of a model, whose norm comes later).
     """
-    import torch
     lib = _lib()
+    f16 = _state["f16"]
     if h.dim() != 2:
         raise ValueError("h must be [rows][cols]")
     n, cols = h.shape
-    f16 = _state["f16"]
-    a = _Norm()
-    a.n_rows, a.n_cols, a.res_scale, a.eps = n, cols, res_scale, eps
-    a.h, a.h_ld, a.h_type = _typed_rows(h, "h", n, cols)
+    hp, h_ld, h_type = _typed_rows(h, "h", n, cols)
+    yp = y_ld = y_type = hop = ho_ld = pw = gp = g_ld = wp = xp = x_ld = 0
     if y is not None:
-        a.y, a.y_ld, a.y_type = _typed_rows(y, "y", n, cols)
-        if h_out is None or h_out is h:
-            a.h_out, a.h_out_ld = a.h, a.h_ld
-        else:
-            a.h_out, a.h_out_ld = _rows(h_out, h.dtype, "h_out", n, cols)
+        yp, y_ld, y_type = _typed_rows(y, "y", n, cols)
+        hop, ho_ld = (hp, h_ld) if h_out is None or h_out is h else _rows(h_out, h.dtype, "h_out", n, cols)
         if post_weight is not None:
-            a.post_weight = _array(post_weight, (f16,), "post_weight", (cols,))
+            pw = _array(post_weight, f16, "post_weight", (cols,))
         if gate is not None:
             if gate.dim() == 1:
-                a.gate = _array(gate, (f16,), "gate", (cols,))
+                gp = _array(gate, f16, "gate", (cols,))
             else:
-                a.gate, a.gate_ld = _rows(gate, f16, "gate", n, cols)
+                gp, g_ld = _rows(gate, f16, "gate", n, cols)
     elif post_weight is not None or gate is not None or h_out is not None:
         raise ValueError("post_weight, gate and h_out go with y")
     if want_x:
         if weight is None:
             raise ValueError("x needs weight")
-        a.weight = _array(weight, (f16,), "weight", (cols,))
+        wp = _array(weight, f16, "weight", (cols,))
         if x is None:
+            import torch
             x = torch.empty((n, cols), dtype=f16, device=h.device)
-        a.x, a.x_ld = _rows(x, f16, "x", n, cols)
+        xp, x_ld = _rows(x, f16, "x", n, cols)
     elif y is None:
         raise ValueError("nothing to do without y and x")
     else:
         x = None
-    rc = lib.qtea_norm(ctypes.addressof(a), _stream_of(stream, h.device.index))
+    args = _NORM.pack(hp, yp, pw, gp, wp, hop, xp, h_ld, y_ld, g_ld, ho_ld, x_ld, h_type, y_type, n, cols, res_scale, eps)
+    rc = lib.qtea_norm(args, _stream_of(stream, h.get_device()))
     if rc:
         _fail(rc, "qtea_norm")
     return x

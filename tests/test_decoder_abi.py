@@ -27,7 +27,7 @@ def test_kv_create_refuses_before_it_looks_for_a_device():
 def test_calls_without_a_cache_are_refused():
     lib = qt.load()
     b = ctypes.byref(d._Batch(P, P, P, 1, 1, 1, 1))
-    assert lib.qtea_kv_append(None, b, ctypes.byref(d._Append()), None) == BAD
+    assert lib.qtea_kv_append(None, b, bytes(d._APPEND.size), None) == BAD
     assert lib.qtea_kv_read(None, b, P, 1, P, P, None) == BAD
     assert lib.qtea_attention(None, b, P, 64, 1, 1.0, 0, P, 64, None, P, 1 << 30, None) == BAD
     assert lib.qtea_attention_workspace(None) == BAD
@@ -36,11 +36,10 @@ def test_calls_without_a_cache_are_refused():
 
 
 def norm(**kw):
-    a = d._Norm(h=256, y=256, post_weight=256, gate=256, weight=256, h_out=256, x=256, h_ld=64, y_ld=64, gate_ld=64,
-                h_out_ld=64, x_ld=64, h_type=0, y_type=0, n_rows=2, n_cols=64, res_scale=1.0, eps=1e-6)
-    for k, v in kw.items():
-        setattr(a, k, v)
-    return qt.load().qtea_norm(ctypes.byref(a), None)
+    a = dict(h=256, y=256, post_weight=256, gate=256, weight=256, h_out=256, x=256, h_ld=64, y_ld=64, gate_ld=64,
+             h_out_ld=64, x_ld=64, h_type=0, y_type=0, n_rows=2, n_cols=64, res_scale=1.0, eps=1e-6)
+    a.update(kw)
+    return qt.load().qtea_norm(d._NORM.pack(*(v or 0 for v in a.values())), None)
 
 
 def test_norm_refusals():
