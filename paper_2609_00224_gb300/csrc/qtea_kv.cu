@@ -31,7 +31,7 @@ struct AppendParams {
 };
 
 constexpr int kAppendWarps = 8;
-constexpr int kAppendPasses = 4;
+constexpr int kAppendPasses = 2;
 
 // Four consecutive elements as fp32: one access where the rows are aligned for it.
 template <int TYPE, bool VEC>
@@ -151,8 +151,8 @@ __global__ void __launch_bounds__(kAppendWarps * 32) qtea_kv_append_kernel(const
       __half* o = p.q_out + ((long long)t * p.q_heads + head) * D + 4 * l;
       const uint2 x = half4(a[i]), y = half4(b[i]);
       if (VEC) {
-        *reinterpret_cast<uint2*>(o) = x;
-        *reinterpret_cast<uint2*>(o + D / 2) = y;
+        __stcs(reinterpret_cast<uint2*>(o), x);
+        __stcs(reinterpret_cast<uint2*>(o + D / 2), y);
       } else {
         reinterpret_cast<uint32_t*>(o)[0] = x.x, reinterpret_cast<uint32_t*>(o)[1] = x.y;
         reinterpret_cast<uint32_t*>(o + D / 2)[0] = y.x, reinterpret_cast<uint32_t*>(o + D / 2)[1] = y.y;
@@ -166,8 +166,8 @@ __global__ void __launch_bounds__(kAppendWarps * 32) qtea_kv_append_kernel(const
       if (store) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) a[i][e] = saturate_f16(a[i][e]), b[i][e] = saturate_f16(b[i][e]);
-        reinterpret_cast<uint2*>(dst)[l] = half4(a[i]);
-        reinterpret_cast<uint2*>(dst)[D / 8 + l] = half4(b[i]);
+        __stcs(reinterpret_cast<uint2*>(dst) + l, half4(a[i]));
+        __stcs(reinterpret_cast<uint2*>(dst) + D / 8 + l, half4(b[i]));
       }
       continue;
     }
@@ -192,8 +192,8 @@ __global__ void __launch_bounds__(kAppendWarps * 32) qtea_kv_append_kernel(const
 #pragma unroll
     for (int e = 0; e < 4; ++e) a[i][e] *= fa, b[i][e] *= fb;
     if (FMT == QTEA_KV_FP8) {
-      reinterpret_cast<uint32_t*>(dst)[l] = to_e4m3x2(a[i][0], a[i][1]) | to_e4m3x2(a[i][2], a[i][3]) << 16;
-      reinterpret_cast<uint32_t*>(dst)[D / 8 + l] = to_e4m3x2(b[i][0], b[i][1]) | to_e4m3x2(b[i][2], b[i][3]) << 16;
+      __stcs(reinterpret_cast<uint32_t*>(dst) + l, to_e4m3x2(a[i][0], a[i][1]) | to_e4m3x2(a[i][2], a[i][3]) << 16);
+      __stcs(reinterpret_cast<uint32_t*>(dst) + D / 8 + l, to_e4m3x2(b[i][0], b[i][1]) | to_e4m3x2(b[i][2], b[i][3]) << 16);
     } else {
       reinterpret_cast<uint16_t*>(dst)[l] = (uint16_t)(to_e2m1x2(a[i][0], a[i][1]) | to_e2m1x2(a[i][2], a[i][3]) << 8);
       reinterpret_cast<uint16_t*>(dst)[D / 8 + l] =
