@@ -135,9 +135,14 @@ __device__ __forceinline__ uint4 lds128(uint32_t a) {
   asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a) : "memory");
   return v;
 }
-__device__ __forceinline__ uint32_t lds8(uint32_t a) {
+__device__ __forceinline__ uint32_t lds32(uint32_t a) {
   uint32_t r;
-  asm volatile("ld.shared.u8 %0, [%1];" : "=r"(r) : "r"(a) : "memory");
+  asm volatile("ld.shared.u32 %0, [%1];" : "=r"(r) : "r"(a) : "memory");
+  return r;
+}
+__device__ __forceinline__ uint32_t lds16(uint32_t a) {
+  uint16_t r;
+  asm volatile("ld.shared.u16 %0, [%1];" : "=h"(r) : "r"(a) : "memory");
   return r;
 }
 __device__ __forceinline__ void fence_async_shared() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
@@ -178,6 +183,14 @@ __device__ __forceinline__ float2 add2(float2 a, float2 b) {
 __device__ __forceinline__ uint64_t operand(uint32_t addr, uint32_t lead) {
   return (uint64_t)((addr & 0x3ffffu) >> 4) | (uint64_t)(lead >> 4) << 16 | (uint64_t)(1024u >> 4) << 32 | 1ull << 46 |
          2ull << 61;
+}
+
+// One lane of the warp, the same one each time; the compiler knows that what it guards runs in one lane and
+// keeps descriptors in uniform registers.
+__device__ __forceinline__ bool elect_one() {
+  uint32_t r;
+  asm volatile("{ .reg .pred p; elect.sync _|p, 0xffffffff; selp.u32 %0, 1, 0, p; }" : "=r"(r));
+  return r != 0;
 }
 
 template <int FMT, int D>
@@ -348,6 +361,7 @@ __global__ void __launch_bounds__((Chunk<FMT, D>::kThreads), 1)
       constexpr uint32_t kIdescO = 1u << 4 | 1u << 16 | (D >> 3) << 17 | (kRowsTile >> 4) << 24;
       uint32_t stage = 0, phase = 0;
       uint32_t q_phase = 0, o_phase = 1, p_phase[2] = {0, 0};
+      const uint64_t q_desc = operand(q_smem, 16), k_desc = operand(kv_smem, 16), v_desc = operand(kv_smem, T::kPartBytes);
       for (int cur = begin; cur < end;) {
         const AttnItem it = attn_item(p, tab, cur, end);
         cur = it.next;
@@ -358,18 +372,19 @@ __global__ void __launch_bounds__((Chunk<FMT, D>::kThreads), 1)
         wait(sh.q_full, q_phase);
         q_phase ^= 1;
         auto release = [&] {  // the stage is free when the products issued so far are complete
-          if (lane == 0) mma_commit(smem_u32(&sh.empty[stage]));
+          if (elect_one()) mma_commit(smem_u32(&sh.empty[stage]));
           __syncwarp();
           if (++stage == T::kStages) stage = 0, phase ^= 1;
         };
         auto scores = [&](int g, int q_tile) {  // S_g = Q K^T
           tmem_fence_after();
-          if (lane == 0) {
-            const uint32_t qa = q_smem + q_tile * T::kTileBytes, kb = kv_smem + stage * T::kTileBytes;
+          const uint64_t qd = q_desc + q_tile * (T::kTileBytes >> 4), kd = k_desc + stage * (T::kTileBytes >> 4);
+          if (elect_one()) {
 #pragma unroll
             for (int k = 0; k < D / 16; ++k) {
-              const uint32_t at = (k >> 2) * T::kPartBytes + (k & 3) * 32;
-              mma_ss(tmem + g * 128, operand(qa + at, 16), operand(kb + at, 16), kIdescS, k > 0);
+              constexpr int kPart = T::kPartBytes >> 4;
+              const int at = (k >> 2) * kPart + (k & 3) * 2;  // 16 elements on: 32 bytes of a row
+              mma_ss(tmem + g * 128, qd + at, kd + at, kIdescS, k > 0);
             }
             mma_commit(smem_u32(&sh.s_full[g]));
           }
@@ -392,19 +407,18 @@ __global__ void __launch_bounds__((Chunk<FMT, D>::kThreads), 1)
           wait(sh.p_full[g], p_phase[g]);
           p_phase[g] ^= 1;
           tmem_fence_after();
-          if (lane == 0) {
-            const uint32_t vb = kv_smem + stage * T::kTileBytes;
+          const uint64_t vd = v_desc + stage * (T::kTileBytes >> 4);
+          if (elect_one()) {
 #pragma unroll
-            for (int k = 0; k < kUnit / 16; ++k)
-              mma_ts(tmem + 256 + g * 128, tmem + g * 128 + k * 8, operand(vb + k * 2048, T::kPartBytes), kIdescO,
-                     accumulate || k > 0);
+            for (int k = 0; k < kUnit / 16; ++k)  // 16 keys on: 2048 bytes
+              mma_ts(tmem + 256 + g * 128, tmem + g * 128 + k * 8, vd + k * 128, kIdescO, accumulate || k > 0);
             if (last) mma_commit(smem_u32(&sh.o_full[g]));
           }
           __syncwarp();
         };
         auto next_full = [&] { wait(sh.full[stage], phase); };
         auto q_done = [&] {
-          if (lane == 0) mma_commit(smem_u32(&sh.q_empty));
+          if (elect_one()) mma_commit(smem_u32(&sh.q_empty));
           __syncwarp();
         };
         auto o_ready = [&] {  // the previous item's accumulators have been read
@@ -524,36 +538,40 @@ __global__ void __launch_bounds__((Chunk<FMT, D>::kThreads), 1)
         const uint32_t src = raw_smem + raw * T::kRawBytes, sc = src + kUnit * T::kRawRow;
         const uint32_t dst = kv_smem + stage * T::kTileBytes;
         const bool edge = value && (key0 < in.lo || key0 + kUnit > in.hi);
-        constexpr int kChunks = T::kRawRow / 16;  // 16-byte pieces of a row
-#pragma unroll 4
-        for (int j = 0; j < kChunks; ++j) {
-          const int at = tid + 128 * j, r = at / kChunks, ch = at % kChunks;
-          const uint4 x = lds128(src + at * 16);
-          const bool zero = edge && (key0 + r < in.lo || key0 + r >= in.hi);
-          if (FMT == QTEA_KV_FP8) {
-            const uint32_t f = scale_bits(lds8(sc + r * T::kScaleRow + (ch >> 1))) * 0x10001u;
-            uint32_t o[8];
-            const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+        // A thread takes the row of its number, its 16-byte pieces in an order turned by the row, so that
+        // eight neighbouring lanes read and write different banks: the tile's rows are turned by the
+        // swizzle on one side and lie a multiple of 32 banks apart, or half of it, on the other.
+        constexpr int kPieces = T::kRawRow / 16;
+        const int r = tid, turn = FMT == QTEA_KV_FP4 ? (D == 128 ? r >> 1 : 0) : r;
+        const bool zero = edge && (key0 + r < in.lo || key0 + r >= in.hi);
+        uint4 x[kPieces];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              o[2 * k] = zero ? 0u : hmul2(from_e4m3x2(w[k]), f);
-              o[2 * k + 1] = zero ? 0u : hmul2(from_e4m3x2_hi(w[k]), f);
-            }
-            const uint32_t to = dst + (ch >> 2) * T::kPartBytes + r * 128;
-            const int c0 = (ch & 3) * 2;
-            sts128(to + ((c0 ^ (r & 7)) << 4), make_uint4(o[0], o[1], o[2], o[3]));
-            sts128(to + (((c0 + 1) ^ (r & 7)) << 4), make_uint4(o[4], o[5], o[6], o[7]));
+        for (int j = 0; j < kPieces; ++j) {
+          const int ch = (turn + j) % kPieces;
+          x[j] = zero ? make_uint4(0, 0, 0, 0) : lds128(src + r * T::kRawRow + ch * 16);
+        }
+        uint32_t scale = 0x7f7f7f7fu;
+        if (!zero) scale = D == 128 ? lds32(sc + r * 4) : lds16(sc + r * 2);
+        const uint32_t to = dst + r * 128;
+#pragma unroll
+        for (int j = 0; j < kPieces; ++j) {
+          const int ch = (turn + j) % kPieces;
+          const uint32_t w[4] = {x[j].x, x[j].y, x[j].z, x[j].w};
+          if (FMT == QTEA_KV_FP8) {
+            const uint32_t f = scale_bits(scale >> (ch >> 1) * 8 & 255u) * 0x10001u;
+            const uint32_t at = to + (ch >> 2) * T::kPartBytes, c0 = ((ch & 3) * 2) ^ (r & 7);
+            sts128(at + (c0 << 4), make_uint4(hmul2(from_e4m3x2(w[0]), f), hmul2(from_e4m3x2_hi(w[0]), f),
+                                              hmul2(from_e4m3x2(w[1]), f), hmul2(from_e4m3x2_hi(w[1]), f)));
+            sts128(at + ((c0 ^ 1) << 4), make_uint4(hmul2(from_e4m3x2(w[2]), f), hmul2(from_e4m3x2_hi(w[2]), f),
+                                                    hmul2(from_e4m3x2(w[3]), f), hmul2(from_e4m3x2_hi(w[3]), f)));
           } else {
-            const uint32_t f = scale_bits(lds8(sc + r * T::kScaleRow + ch)) * 0x10001u;
-            const uint32_t to = dst + (ch >> 1) * T::kPartBytes + r * 128;
-            const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+            const uint32_t f = scale_bits(scale >> ch * 8 & 255u) * 0x10001u;
+            const uint32_t at = to + (ch >> 1) * T::kPartBytes, c0 = ((ch & 1) * 4) ^ (r & 7);
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
               uint32_t o[4];
               from_e2m1x8(w[k], o);
-#pragma unroll
-              for (int e = 0; e < 4; ++e) o[e] = zero ? 0u : hmul2(o[e], f);
-              sts128(to + ((((ch & 1) * 4 + k) ^ (r & 7)) << 4), make_uint4(o[0], o[1], o[2], o[3]));
+              sts128(at + ((c0 ^ k) << 4), make_uint4(hmul2(o[0], f), hmul2(o[1], f), hmul2(o[2], f), hmul2(o[3], f)));
             }
           }
         }
