@@ -87,18 +87,6 @@ __device__ __forceinline__ uint32_t lds16(uint32_t a) {
   return r;
 }
 
-// A row's scale bytes as the high bytes of the fp16 powers of two that they stand for (113..142, the
-// exponents -14..15; their top bits are clear).
-__device__ __forceinline__ uint32_t scale_high(uint32_t w) { return ((w & 0x1f1f1f1fu) ^ 0x10101010u) << 2; }
-
-// Block `blk` of two such words as a pair of fp16; a selector with its own top bit set gives a byte of copies
-// of the selected byte's top bit: zeros.
-__device__ __forceinline__ uint32_t scale_pair(uint32_t h0, uint32_t h1, int blk) {
-  uint32_t r;
-  asm("prmt.b32 %0, %1, %2, %3;" : "=r"(r) : "r"(h0), "r"(h1), "r"((8 | blk) | blk << 4 | (12 | blk) << 8 | (4 | blk) << 12));
-  return r;
-}
-
 // The power of two of block `blk` of a row's scale word, as fp32: the byte is its exponent.
 __device__ __forceinline__ float scale_of(uint32_t w, int blk) {
   return __uint_as_float((blk == 3 ? w >> 1 : w << (23 - 8 * blk)) & 0x7f800000u);

@@ -145,6 +145,15 @@ __device__ __forceinline__ uint32_t lds16(uint32_t a) {
   asm volatile("ld.shared.u16 %0, [%1];" : "=h"(r) : "r"(a) : "memory");
   return r;
 }
+// Whether the phase with the given parity has completed, without waiting.
+__device__ __forceinline__ bool mbar_test(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile("{ .reg .pred p; mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2; selp.u32 %0, 1, 0, p; }"
+               : "=r"(ok)
+               : "r"(bar), "r"(parity)
+               : "memory");
+  return ok != 0;
+}
 __device__ __forceinline__ void fence_async_shared() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 template <int ID>
 __device__ __forceinline__ void named_barrier(int threads) {
@@ -202,24 +211,25 @@ struct Chunk {
   static constexpr int kStages = kQuant ? (D == 128 ? 3 : 4) : (D == 128 ? 4 : 8);
   static constexpr int kRawRow = FMT == QTEA_KV_FP8 ? D : D / 2;  // bytes of a quantised row
   static constexpr int kScaleRow = D / kKvBlock;
-  static constexpr int kRawBytes = kQuant ? kUnit * (kRawRow + kScaleRow) : 0;
+  static constexpr int kRawBytes = kQuant ? kUnit * kRawRow : 0;
+  static constexpr int kScaleBytes = kQuant ? kUnit * kScaleRow : 0;
   static constexpr int kRawStages = kQuant ? (FMT == QTEA_KV_FP8 ? 3 : 6) : 0;
-  static constexpr int kSmem = 2 * kTileBytes + kStages * kTileBytes + kRawStages * kRawBytes + 1024;
+  static constexpr int kSmem = 2 * kTileBytes + kStages * kTileBytes + kRawStages * (kRawBytes + kScaleBytes) + 1024;
   static constexpr bool kMaxFirst = kQuant;
   static constexpr int kThreads = kQuant ? 512 : 384;
   // warps: 0-7 softmax, then (quantised) 8-11 conversion, then the four of the last group
   static constexpr int kLast = kThreads / 32 - 4;
-  static constexpr int kCopyWarp = kLast, kMmaWarp = kLast + 1, kQWarp = kLast + 2;
+  static constexpr int kCopyWarp = kLast, kMmaWarp = kLast + 1, kQWarp = kLast + 2, kCopyWarp2 = kLast + 3;
 };
 
 struct ChunkShared {
-  uint64_t full[8], empty[8];          // stages of K and V
+  uint64_t full[9], empty[9];          // stages of K and V
   uint64_t raw_full[6], raw_empty[6];  // stages of quantised rows
   uint64_t q_full, q_empty, o_free;
   uint64_t s_full[2], p_full[2], o_full[2];
   uint32_t tmem;
   int is_last;
-  float m1[2][kRowsTile], l1[2][kRowsTile];  // the second group's rows, where both share them; by items' parity
+  float2 stat[2][2][kRowsTile];  // m and l of each group's rows, by items' parity
 };
 
 // A step of the copies' order. With two row tiles: K0 V0 K1 V1 ..; with one: K0 K1 V0 K2 V1 ...
@@ -273,10 +283,13 @@ __global__ void __launch_bounds__((Chunk<FMT, D>::kThreads), 1)
   const AttnParams& p = cp.a;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t smem = (smem_u32(smem_raw) + 1023u) & ~1023u;
-  const uint32_t q_smem = smem, kv_smem = smem + 2 * T::kTileBytes, raw_smem = kv_smem + T::kStages * T::kTileBytes;
+  // with one row tile the second tile of queries is a stage more
+  const uint32_t stages = cp.two ? T::kStages : T::kStages + 1;
+  const uint32_t q_smem = smem, kv_smem = smem + (cp.two ? 2 : 1) * T::kTileBytes;
+  const uint32_t raw_smem = kv_smem + stages * T::kTileBytes, sc_smem = raw_smem + T::kRawStages * T::kRawBytes;
 
   if (threadIdx.x == 0) {
-    for (int i = 0; i < T::kStages; ++i) {
+    for (int i = 0; i < T::kStages + 1; ++i) {
       mbar_init(smem_u32(&sh.full[i]), T::kQuant ? 4 : 1);
       mbar_init(smem_u32(&sh.empty[i]), 1);
     }
@@ -313,38 +326,46 @@ __global__ void __launch_bounds__((Chunk<FMT, D>::kThreads), 1)
 
   if (warp >= T::kLast) {
     
-    if (warp == T::kCopyWarp) {
+    if (warp == T::kCopyWarp || warp == T::kCopyWarp2) {
       // ------------------------------------------------------------------ copies of keys and values
+      // Two warps take every second step each: one copy takes a lane about 100 clocks to issue.
       const int box = min(p.kv.page_size, kUnit), boxes = kUnit / box;  // tokens of a copy, copies of a unit
-      uint32_t stage = 0, phase = 1;  // the first wait of every stage passes
+      const uint32_t ring = T::kQuant ? T::kRawStages : stages;
+      const int mine = warp == T::kCopyWarp ? 0 : 1;
+      uint32_t stage = mine, phase = 1;  // the first wait of every stage passes
       for (int cur = begin; cur < end;) {
         const AttnItem it = attn_item(p, tab, cur, end);
         cur = it.next;
         if (it.units == 0) continue;
         const int* pages = p.b.pages + (long long)it.s * p.b.max_pages;
         const Order order{it.units, cp.two};
-        for (int i = 0; i < order.steps(); ++i) {
+        const int key_item = it.unit0 * kUnit + box * lane;
+        // the page of this lane's box in step i's unit, looked up two of this warp's steps ahead
+        auto page_of = [&](int i) {
+          if (lane >= boxes || i >= order.steps()) return 0;
           int unit;
           bool value;
           order.at(i, &unit, &value);
-          int row = 0;
-          if (lane < boxes) {
-            const int key = (it.unit0 + unit) * kUnit + box * lane;
-            const int page = __ldg(pages + min(key >> p.kv.page_shift, p.b.max_pages - 1));
-            row = (min(max(page, 0), p.kv.n_pages - 1) * p.kv.heads + it.head) * p.kv.page_size +
-                  (key & (p.kv.page_size - 1));
-          }
+          return __ldg(pages + min((key_item + unit * kUnit) >> p.kv.page_shift, p.b.max_pages - 1));
+        };
+        int ahead[2] = {page_of(mine), page_of(mine + 2)};
+        for (int i = mine; i < order.steps(); i += 2) {
+          int unit;
+          bool value;
+          order.at(i, &unit, &value);
+          const int key = key_item + unit * kUnit, page = min(max(ahead[0], 0), p.kv.n_pages - 1);
+          const int row = (page * p.kv.heads + it.head) * p.kv.page_size + (key & (p.kv.page_size - 1));
+          ahead[0] = ahead[1], ahead[1] = page_of(i + 4);
           if (!wait(T::kQuant ? sh.raw_empty[stage] : sh.empty[stage], phase)) break;
           const uint32_t bar = smem_u32(T::kQuant ? &sh.raw_full[stage] : &sh.full[stage]);
-          if (lane == 0) mbar_arrive_expect_tx(bar, T::kQuant ? T::kRawBytes : T::kTileBytes);
+          if (lane == 0) mbar_arrive_expect_tx(bar, T::kQuant ? T::kRawBytes + T::kScaleBytes : T::kTileBytes);
           __syncwarp();
           if (lane < boxes) {
             if (T::kQuant) {
-              const uint32_t dst = raw_smem + stage * T::kRawBytes;
-              bulk_load(dst + lane * box * T::kRawRow, (value ? p.kv.v : p.kv.k) + (long long)row * T::kRawRow,
-                        box * T::kRawRow, bar);
-              bulk_load(dst + kUnit * T::kRawRow + lane * box * T::kScaleRow,
-                        (value ? p.kv.vs : p.kv.ks) + (long long)row * T::kScaleRow, box * T::kScaleRow, bar);
+              const uint32_t dst = raw_smem + stage * T::kRawBytes, sc = sc_smem + stage * T::kScaleBytes;
+              tma_load_2d(dst + lane * box * T::kRawRow, value ? &map_v : &map_k, 0, row, bar);
+              bulk_load(sc + lane * box * T::kScaleRow, (value ? p.kv.vs : p.kv.ks) + (long long)row * T::kScaleRow,
+                        box * T::kScaleRow, bar);
             } else {
               const uint32_t dst = kv_smem + stage * T::kTileBytes + lane * box * 128;
 #pragma unroll
@@ -352,7 +373,8 @@ __global__ void __launch_bounds__((Chunk<FMT, D>::kThreads), 1)
                 tma_load_2d(dst + h * T::kPartBytes, value ? &map_v : &map_k, h * 128, row, bar);
             }
           }
-          if (++stage == (T::kQuant ? T::kRawStages : T::kStages)) stage = 0, phase ^= 1;
+          stage += 2;
+          if (stage >= ring) stage -= ring, phase ^= 1;
         }
       }
     } else if (warp == T::kMmaWarp) {
@@ -374,7 +396,7 @@ __global__ void __launch_bounds__((Chunk<FMT, D>::kThreads), 1)
         auto release = [&] {  // the stage is free when the products issued so far are complete
           if (elect_one()) mma_commit(smem_u32(&sh.empty[stage]));
           __syncwarp();
-          if (++stage == T::kStages) stage = 0, phase ^= 1;
+          if (++stage == stages) stage = 0, phase ^= 1;
         };
         auto scores = [&](int g, int q_tile) {  // S_g = Q K^T
           tmem_fence_after();
@@ -439,7 +461,7 @@ __global__ void __launch_bounds__((Chunk<FMT, D>::kThreads), 1)
             values(0, j > 0, j == n - 1);
             if (j + 1 < n) {
               const uint32_t vs = stage, vp = phase;
-              if (++stage == T::kStages) stage = 0, phase ^= 1;
+              if (++stage == stages) stage = 0, phase ^= 1;
               next_full();
               scores(0, 0);
               stage = vs, phase = vp;
@@ -519,7 +541,13 @@ __global__ void __launch_bounds__((Chunk<FMT, D>::kThreads), 1)
     }
   } else if (T::kQuant && warp >= 8) {
     // ------------------------------------------------------------------ quantised rows to fp16 tiles
-    const int tid = threadIdx.x - 256;
+    // A thread takes a row, whose 16-byte pieces lie swizzled on both sides: neighbouring lanes read and write
+    // different banks, at places that differ from the row's by a constant bit pattern.
+    constexpr int kPieces = T::kRawRow / 16;
+    constexpr uint32_t kTurn = T::kRawRow == 128 ? 7 : T::kRawRow == 64 ? 3 : 1;
+    const int r = threadIdx.x - 256;
+    const uint32_t from = raw_smem + r * T::kRawRow, turn = ((uint32_t)(r * T::kRawRow) >> 7 & kTurn) << 4;
+    const uint32_t to_turn = (uint32_t)(r & 7) << 4;
     uint32_t stage = 0, phase = 1, raw = 0, raw_phase = 0;
     for (int cur = begin; cur < end;) {
       const AttnItem it = attn_item(p, tab, cur, end);
@@ -527,62 +555,65 @@ __global__ void __launch_bounds__((Chunk<FMT, D>::kThreads), 1)
       if (it.units == 0) continue;
       const Bounds in = item_bounds(p, it);
       const Order order{it.units, cp.two};
-      for (int i = 0; i < order.steps() && ok; ++i) {
+      uint4 x[kPieces];
+      uint32_t scale;
+      auto load = [&](int i) {  // step i's row, zeros where nothing sees it
         int unit;
         bool value;
         order.at(i, &unit, &value);
-        const int key0 = (it.unit0 + unit) * kUnit;
-        wait(sh.raw_full[raw], raw_phase);
+        const int key = (it.unit0 + unit) * kUnit + r;
+#pragma unroll
+        for (int j = 0; j < kPieces; ++j) x[j] = lds128(from + raw * T::kRawBytes + ((uint32_t)(j << 4) ^ turn));
+        const uint32_t sc = sc_smem + raw * T::kScaleBytes;
+        scale = D == 128 ? lds32(sc + r * 4) : lds16(sc + r * 2);
+        if (value && (key < in.lo || key >= in.hi)) {
+          scale = 0x7f7f7f7fu;
+#pragma unroll
+          for (int j = 0; j < kPieces; ++j) x[j] = make_uint4(0, 0, 0, 0);
+        }
+      };
+      bool loaded = false;
+      for (int i = 0; i < order.steps() && ok; ++i) {
+        if (!loaded) {
+          wait(sh.raw_full[raw], raw_phase);
+          load(i);
+        }
         wait(sh.empty[stage], phase);
         if (!ok) break;
-        const uint32_t src = raw_smem + raw * T::kRawBytes, sc = src + kUnit * T::kRawRow;
-        const uint32_t dst = kv_smem + stage * T::kTileBytes;
-        const bool edge = value && (key0 < in.lo || key0 + kUnit > in.hi);
-        // A thread takes the row of its number, its 16-byte pieces in an order turned by the row, so that
-        // eight neighbouring lanes read and write different banks: the tile's rows are turned by the
-        // swizzle on one side and lie a multiple of 32 banks apart, or half of it, on the other.
-        constexpr int kPieces = T::kRawRow / 16;
-        const int r = tid, turn = FMT == QTEA_KV_FP4 ? (D == 128 ? r >> 1 : 0) : r;
-        const bool zero = edge && (key0 + r < in.lo || key0 + r >= in.hi);
-        uint4 x[kPieces];
+        const uint32_t to = kv_smem + stage * T::kTileBytes + r * 128, high = scale_high(scale);
 #pragma unroll
         for (int j = 0; j < kPieces; ++j) {
-          const int ch = (turn + j) % kPieces;
-          x[j] = zero ? make_uint4(0, 0, 0, 0) : lds128(src + r * T::kRawRow + ch * 16);
-        }
-        uint32_t scale = 0x7f7f7f7fu;
-        if (!zero) scale = D == 128 ? lds32(sc + r * 4) : lds16(sc + r * 2);
-        const uint32_t to = dst + r * 128;
-#pragma unroll
-        for (int j = 0; j < kPieces; ++j) {
-          const int ch = (turn + j) % kPieces;
           const uint32_t w[4] = {x[j].x, x[j].y, x[j].z, x[j].w};
           if (FMT == QTEA_KV_FP8) {
-            const uint32_t f = scale_bits(scale >> (ch >> 1) * 8 & 255u) * 0x10001u;
-            const uint32_t at = to + (ch >> 2) * T::kPartBytes, c0 = ((ch & 3) * 2) ^ (r & 7);
-            sts128(at + (c0 << 4), make_uint4(hmul2(from_e4m3x2(w[0]), f), hmul2(from_e4m3x2_hi(w[0]), f),
-                                              hmul2(from_e4m3x2(w[1]), f), hmul2(from_e4m3x2_hi(w[1]), f)));
-            sts128(at + ((c0 ^ 1) << 4), make_uint4(hmul2(from_e4m3x2(w[2]), f), hmul2(from_e4m3x2_hi(w[2]), f),
-                                                    hmul2(from_e4m3x2(w[3]), f), hmul2(from_e4m3x2_hi(w[3]), f)));
+            const uint32_t f = scale_pair(high, high, j >> 1), at = to + (j >> 2) * T::kPartBytes;
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+              sts128(at + ((uint32_t)((j & 3) * 32 + k * 16) ^ to_turn),
+                     make_uint4(hmul2(from_e4m3x2(w[2 * k]), f), hmul2(from_e4m3x2_hi(w[2 * k]), f),
+                                hmul2(from_e4m3x2(w[2 * k + 1]), f), hmul2(from_e4m3x2_hi(w[2 * k + 1]), f)));
           } else {
-            const uint32_t f = scale_bits(scale >> ch * 8 & 255u) * 0x10001u;
-            const uint32_t at = to + (ch >> 1) * T::kPartBytes, c0 = ((ch & 1) * 4) ^ (r & 7);
+            const uint32_t f = scale_pair(high, high, j), at = to + (j >> 1) * T::kPartBytes;
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
               uint32_t o[4];
               from_e2m1x8(w[k], o);
-              sts128(at + ((c0 ^ k) << 4), make_uint4(hmul2(o[0], f), hmul2(o[1], f), hmul2(o[2], f), hmul2(o[3], f)));
+              sts128(at + ((uint32_t)((j & 1) * 64 + k * 16) ^ to_turn),
+                     make_uint4(hmul2(o[0], f), hmul2(o[1], f), hmul2(o[2], f), hmul2(o[3], f)));
             }
           }
         }
+        const uint32_t done = raw;
+        if (++raw == T::kRawStages) raw = 0, raw_phase ^= 1;
+        // the next row is on its way, where its copy has landed, while this one's stores are made known
+        loaded = i + 1 < order.steps() && __all_sync(0xffffffffu, mbar_test(smem_u32(&sh.raw_full[raw]), raw_phase));
+        if (loaded) load(i + 1);
         fence_async_shared();
         __syncwarp();
         if (lane == 0) {
           mbar_arrive(smem_u32(&sh.full[stage]));
-          mbar_arrive(smem_u32(&sh.raw_empty[raw]));
+          mbar_arrive(smem_u32(&sh.raw_empty[done]));
         }
-        if (++stage == T::kStages) stage = 0, phase ^= 1;
-        if (++raw == T::kRawStages) raw = 0, raw_phase ^= 1;
+        if (++stage == stages) stage = 0, phase ^= 1;
       }
     }
   } else {
@@ -593,19 +624,19 @@ __global__ void __launch_bounds__((Chunk<FMT, D>::kThreads), 1)
     const uint32_t s_addr = lanes + g * 128, o_addr = lanes + 256 + g * 128;
     uint32_t s_phase = 0, o_phase = 0, odd = 0;
     for (int cur = begin, next = begin; cur < end; cur = next) {
-      int unit0, n, steps, hi, lo, hi_in, lo_in;
+      int unit0, steps, hi, hi_in, lo_in;
       bool live;  // a row of the item (the tile may have others, and its lanes then hold anything)
       {
         const AttnItem it = attn_item(p, tab, cur, end);
         next = it.next;
         if (it.units == 0) continue;
-        n = it.units, unit0 = it.unit0;
+        unit0 = it.unit0;
         const int t0 = it.tile * p.tile_tokens + (cp.two ? g * cp.half_tokens : 0);
         const int tokens = max(0, min(min(it.seq.n - t0, cp.half_tokens), p.tile_tokens));
         live = row < tokens * p.group;
-        steps = cp.two ? (tokens > 0 ? n : 0) : (n + 1 - g) >> 1;
+        steps = cp.two ? (tokens > 0 ? it.units : 0) : (it.units + 1 - g) >> 1;
         const int first = it.seq.base + t0, last = first + tokens - 1, pos = first + attn_token(p, row);
-        hi = pos + 1, lo = p.window > 0 ? max(0, pos - p.window + 1) : 0;
+        hi = pos + 1;  // the row sees keys before it and, with a window, from hi - window
         // keys that all of the group's rows see: units inside need no mask
         hi_in = first + 1, lo_in = p.window > 0 ? max(0, last - p.window + 1) : 0;
       }
@@ -620,7 +651,7 @@ __global__ void __launch_bounds__((Chunk<FMT, D>::kThreads), 1)
           if (masked) {
 #pragma unroll
             for (int e = 0; e < 32; ++e)
-              if (key0 + k0 + e >= hi || key0 + k0 + e < lo) s[e] = kNegInf;
+              if (key0 + k0 + e >= hi || (p.window > 0 && key0 + k0 + e < hi - p.window)) s[e] = kNegInf;
           }
         };
         // The row's maximum here, a new reference from it where `wanted` says so, and what has been
@@ -687,7 +718,7 @@ __global__ void __launch_bounds__((Chunk<FMT, D>::kThreads), 1)
         } else {
           uint32_t w[kUnit / 2];
           // a reference is wanted in the first unit that a row sees something of
-          if (__any_sync(0xffffffffu, live && m == kNegInf && key0 < hi && key0 + kUnit > lo)) refer(0.f);
+          if (__any_sync(0xffffffffu, live && m == kNegInf && key0 < hi && (p.window == 0 || key0 + kUnit > hi - p.window))) refer(0.f);
           for (;;) {
             sum[0] = sum[1] = make_float2(0.f, 0.f);
             over[0] = over[1] = kNegInf;
@@ -717,28 +748,33 @@ __global__ void __launch_bounds__((Chunk<FMT, D>::kThreads), 1)
         o_phase ^= 1;
       }
       odd ^= 1;
-      if (!cp.two && g == 1) sh.m1[odd][row] = m, sh.l1[odd][row] = l;
+      sh.stat[odd][g][row] = make_float2(m, l);
       named_barrier<1>(256);
       tmem_fence_after();
       const AttnItem it = attn_item(p, tab, cur, end);  // again: not kept over the loop above
       const int t0 = it.tile * p.tile_tokens + (cp.two ? g * cp.half_tokens : 0);
       const int c0 = split.cta_of(it.first), c1 = split.cta_of(it.last);
-      // With one row tile the first group joins both accumulators (the lanes are the same).
-      const bool writer = cp.two ? true : g == 0;
+      // With one row tile both groups' accumulators are of the same rows, on the same lanes: each group joins
+      // half of the columns.
+      const bool both = !cp.two && it.units > 1;
+      const int d0 = cp.two ? 0 : g * (D / 2), d1 = cp.two ? D : d0 + D / 2;
       float fa = 1.f, fb = 0.f;
-      if (!cp.two && g == 0) {
-        const float m1 = sh.m1[odd][row], l1 = sh.l1[odd][row], top = fmaxf(m, m1);
-        fa = top == kNegInf ? 0.f : ex2(m - top);
-        fb = top == kNegInf ? 0.f : ex2(m1 - top);
-        m = top;
-        l = l * fa + l1 * fb;
+      if (!cp.two) {
+        const float2 a = sh.stat[odd][0][row], b = sh.stat[odd][1][row];
+        m = fmaxf(a.x, b.x);
+        fa = m == kNegInf ? 0.f : ex2(a.x - m);
+        fb = m == kNegInf ? 0.f : ex2(b.x - m);
+        l = a.y * fa + b.y * fb;
       }
-      const bool both = !cp.two && n > 1;
+      const float inv = l == 0.f ? 0.f : 1.f / l;
+      fa *= inv, fb *= inv;
+      const bool some = cp.two ? steps > 0 : true;  // whether there are accumulators to read
       const int tok = it.seq.q0 + t0 + attn_token(p, row), head = it.head * p.group + (row - attn_token(p, row) * p.group);
-      const bool mine = writer && live;
-      constexpr size_t kSlot = (size_t)2 * kRowsTile * (128 + 2);  // floats: [D/4][256][4], then m, l
-      float* slot = p.slots + (2 * (size_t)blockIdx.x + ((int)blockIdx.x == c0 ? 1 : 0)) * kSlot;
-      const int slot_row = g * kRowsTile + row;
+      // a partial result: O / l as [D/4][256][4], then m + log2 l
+      constexpr size_t kSlot = (size_t)2 * kRowsTile * (128 + 1);
+      auto slot_of = [&](int cta) { return p.slots + (2 * (size_t)cta + (cta == c0 ? 1 : 0)) * kSlot; };
+      float* slot = slot_of(blockIdx.x);
+      const int slot_row = (cp.two ? g * kRowsTile : 0) + row;
       auto store_row = [&](int d, const float* v) {  // 16 elements of this thread's row, as fp16
         __half* o = p.out + (long long)tok * p.out_ld + (long long)head * D + d;
         uint32_t w[8];
@@ -755,31 +791,27 @@ __global__ void __launch_bounds__((Chunk<FMT, D>::kThreads), 1)
           for (int e = 0; e < 8; ++e) reinterpret_cast<uint32_t*>(o)[e] = w[e];
         }
       };
-      auto store_lse = [&](float top, float total) {
-        if (p.lse)
-          p.lse[(long long)tok * p.q_heads + head] =
-              total > 0.f ? (top + log2f(total)) * 0.6931471805599453f : total == 0.f ? kNegInf : total;
+      auto stat_of = [](float top, float total) {
+        return total > 0.f ? top + log2f(total) : total == 0.f ? kNegInf : total;
       };
-      if (writer && steps > 0) {
-        const float inv = l == 0.f ? 0.f : 1.f / l;
+      auto store_lse = [&](float stat) {
+        if (p.lse && (cp.two || g == 0)) p.lse[(long long)tok * p.q_heads + head] = stat * 0.6931471805599453f;
+      };
+      if (some) {
 #pragma unroll 1
-        for (int d = 0; d < D; d += 16) {
+        for (int d = d0; d < d1; d += 16) {
           uint32_t x[16], y[16];
           float* v = reinterpret_cast<float*>(x);
-          tmem_ld16(x, o_addr + d);
-          if (both) tmem_ld16(y, o_addr + 128 + d);
+          tmem_ld16(x, (cp.two ? o_addr : lanes + 256) + d);
+          if (both) tmem_ld16(y, lanes + 384 + d);
           tmem_wait_ld();
-          if (!cp.two) {
 #pragma unroll
-            for (int e = 0; e < 16; ++e) {
-              v[e] *= fa;
-              if (both) v[e] = fmaf(__uint_as_float(y[e]), fb, v[e]);
-            }
+          for (int e = 0; e < 16; ++e) {
+            v[e] = l == 0.f ? 0.f : v[e] * fa;
+            if (both && l != 0.f) v[e] = fmaf(__uint_as_float(y[e]), fb, v[e]);
           }
           if (c0 == c1) {
-#pragma unroll
-            for (int e = 0; e < 16; ++e) v[e] = l == 0.f ? 0.f : v[e] * inv;
-            if (mine) store_row(d, v);
+            if (live) store_row(d, v);
           } else {
 #pragma unroll
             for (int e = 0; e < 16; e += 4)
@@ -792,12 +824,9 @@ __global__ void __launch_bounds__((Chunk<FMT, D>::kThreads), 1)
       __syncwarp();
       if (lane == 0) mbar_arrive(smem_u32(&sh.o_free));
       if (c0 == c1) {
-        if (mine && steps > 0) store_lse(m, l);
+        if (live) store_lse(stat_of(m, l));
       } else {
-        if (writer) {
-          __stcg(slot + D * 256 + slot_row, m);
-          __stcg(slot + D * 256 + 256 + slot_row, l);
-        }
+        if (cp.two || g == 0) __stcg(slot + D * 256 + slot_row, stat_of(m, l));
         __threadfence();
         named_barrier<1>(256);
         if (threadIdx.x == 0) {
@@ -806,39 +835,52 @@ __global__ void __launch_bounds__((Chunk<FMT, D>::kThreads), 1)
           if (sh.is_last) p.counters[c0] = 0;
         }
         named_barrier<1>(256);
-        if (sh.is_last && mine) {
+        if (sh.is_last && live) {
           __threadfence();
+          // four parts at a time, all of their loads in flight
           const int parts = c1 - c0 + 1;
-          auto part = [&](int i) { return p.slots + (2 * (size_t)(c0 + i) + (i == 0 ? 1 : 0)) * kSlot; };
-          float top = kNegInf, total = 0.f;
-#pragma unroll 4
-          for (int i = 0; i < parts; ++i) top = fmaxf(top, __ldcg(part(i) + D * 256 + slot_row));
-#pragma unroll 4
-          for (int i = 0; i < parts; ++i) {
-            const float f = top == kNegInf ? 0.f : ex2(__ldcg(part(i) + D * 256 + slot_row) - top);
-            total = fmaf(__ldcg(part(i) + D * 256 + 256 + slot_row), f, total);
-          }
-          const float inv = total == 0.f ? 0.f : 1.f / total;
 #pragma unroll 1
-          for (int d = 0; d < D; d += 16) {
-            float v[16];
+          for (int d = d0; d < d1; d += 16) {
+            float v[16], top = kNegInf, total = 0.f;
 #pragma unroll
             for (int e = 0; e < 16; ++e) v[e] = 0.f;
-#pragma unroll 2
-            for (int i = 0; i < parts; ++i) {
-              const float f = top == kNegInf ? 0.f : ex2(__ldcg(part(i) + D * 256 + slot_row) - top);
+#pragma unroll 1
+            for (int i0 = 0; i0 < parts; i0 += 4) {
+              float st[4];
+              float4 x[4][4];
 #pragma unroll
-              for (int e = 0; e < 16; e += 4) {
-                const float4 x = __ldcg(reinterpret_cast<const float4*>(part(i)) + ((d + e) / 4) * 256 + slot_row);
-                v[e] = fmaf(x.x, f, v[e]), v[e + 1] = fmaf(x.y, f, v[e + 1]);
-                v[e + 2] = fmaf(x.z, f, v[e + 2]), v[e + 3] = fmaf(x.w, f, v[e + 3]);
+              for (int i = 0; i < 4; ++i) {
+                const float* part = slot_of(c0 + min(i0 + i, parts - 1));
+                st[i] = i0 + i < parts ? __ldcg(part + D * 256 + slot_row) : kNegInf;
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                  x[i][e] = __ldcg(reinterpret_cast<const float4*>(part) + (d / 4 + e) * 256 + slot_row);
+              }
+              const float next = fmaxf(fmaxf(fmaxf(st[0], st[1]), fmaxf(st[2], st[3])), top);
+              const float ref = next == kNegInf ? 0.f : next, old = ex2(top - ref);
+              top = next;
+              total *= old;
+#pragma unroll
+              for (int e = 0; e < 16; ++e) v[e] *= old;
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                const float f = ex2(st[i] - ref);
+                total += f;
+                if (f != 0.f) {  // a part without keys for this row has not written it
+#pragma unroll
+                  for (int e = 0; e < 4; ++e) {
+                    v[4 * e] = fmaf(x[i][e].x, f, v[4 * e]), v[4 * e + 1] = fmaf(x[i][e].y, f, v[4 * e + 1]);
+                    v[4 * e + 2] = fmaf(x[i][e].z, f, v[4 * e + 2]), v[4 * e + 3] = fmaf(x[i][e].w, f, v[4 * e + 3]);
+                  }
+                }
               }
             }
+            const float scale = total == 0.f ? 0.f : 1.f / total;
 #pragma unroll
-            for (int e = 0; e < 16; ++e) v[e] = total == 0.f ? 0.f : v[e] * inv;
+            for (int e = 0; e < 16; ++e) v[e] *= scale;
             store_row(d, v);
+            if (d == 0) store_lse(stat_of(top, total));
           }
-          store_lse(top, total);
         }
       }
     }
@@ -869,7 +911,7 @@ cudaError_t launch_dim(const qtea_kv* kv, const ChunkParams& cp, const CUtensorM
 }  // namespace
 
 size_t attn_chunk_floats(int sm_count) {
-  return (size_t)std::min(sm_count, kAttnMaxCtas) * 2 * kRowsTile * (128 + 2);
+  return (size_t)std::min(sm_count, kAttnMaxCtas) * 2 * kRowsTile * (128 + 1);
 }
 
 cudaError_t launch_attn_chunk(const qtea_kv* kv, const AttnParams& base, cudaStream_t st) {

@@ -376,9 +376,8 @@ int qtea_kv_create(void* k_pages, void* v_pages, void* k_scales, void* v_scales,
                   swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
   };
   const int unit = 1 << kv_unit_shift(format);
-  bool made = make(&kv->map_k, k_pages, unit) && make(&kv->map_v, v_pages, unit);
-  if (format == QTEA_KV_F16) made = made && make(&kv->wide_k, k_pages, 128) && make(&kv->wide_v, v_pages, 128);
-  if (!made) {
+  if (!make(&kv->map_k, k_pages, unit) || !make(&kv->map_v, v_pages, unit) || !make(&kv->wide_k, k_pages, 128) ||
+      !make(&kv->wide_v, v_pages, 128)) {
     delete kv;
     return QTEA_ERR_CUDA;
   }

@@ -129,6 +129,18 @@ __device__ __forceinline__ uint32_t hmul2(uint32_t a, uint32_t b) {
 // fp16 bits of the power of two that a scale byte stands for (113..142 in a cache that append
 // wrote; other bytes, in rows that nothing wrote, give some fp16 value).
 __device__ __forceinline__ uint32_t scale_bits(uint32_t byte) { return ((byte - 112u) & 31u) << 10; }
+
+// A row's scale bytes as the high bytes of the fp16 powers of two that they stand for (113..142, the
+// exponents -14..15; their top bits are clear).
+__device__ __forceinline__ uint32_t scale_high(uint32_t w) { return ((w & 0x1f1f1f1fu) ^ 0x10101010u) << 2; }
+
+// Block `blk` of two such words as a pair of fp16; a selector with its own top bit set gives a byte of copies
+// of the selected byte's top bit: zeros.
+__device__ __forceinline__ uint32_t scale_pair(uint32_t h0, uint32_t h1, int blk) {
+  uint32_t r;
+  asm("prmt.b32 %0, %1, %2, %3;" : "=r"(r) : "r"(h0), "r"(h1), "r"((8 | blk) | blk << 4 | (12 | blk) << 8 | (4 | blk) << 12));
+  return r;
+}
 #endif
 
 }  // namespace qtea
@@ -138,7 +150,7 @@ struct qtea_kv {
   int device, sm_count;
   void* encode;              // the driver's cuTensorMapEncodeTiled
   // The codes as rows of bytes, in boxes of at most 128 bytes by as many tokens as a unit of the
-  // kernel and a page both hold: few-rows kernel, and (fp16) many-rows kernel.
+  // kernel and a page both hold: few-rows kernel, many-rows kernel.
   CUtensorMap map_k, map_v, wide_k, wide_v;
 };
 
