@@ -143,6 +143,7 @@ __global__ void __launch_bounds__(kWarps * 32, (Rows<FMT, D, NT>::kCtas))
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   const AttnTable tab = attn_table(smem + T::kRing + T::kScaleRing, p.b.n_seqs);
+  attn_begin();
   attn_prefix(p, tab);
   int cur;
   {
@@ -657,11 +658,7 @@ cudaError_t launch(const qtea_kv* kv, const AttnParams& p, cudaStream_t st) {
   const int smem = T::kRing + T::kScaleRing + kAttnTableBytes(p.b.n_seqs);
   const int grid = std::min(T::kCtas * kv->sm_count, kAttnMaxCtas);
   static_assert(kWarps * D * 8 * NT * 4 <= T::kRing, "the joined results fit the rings");
-  auto k = qtea_attn_rows_kernel<FMT, D, NT>;
-  cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
-  if (e != cudaSuccess) return e;
-  k<<<grid, kWarps * 32, smem, st>>>(kv->map_k, kv->map_v, p);
-  return cudaGetLastError();
+  return attn_launch(qtea_attn_rows_kernel<FMT, D, NT>, grid, kWarps * 32, smem, st, kv->map_k, kv->map_v, p);
 }
 
 template <int FMT, int D>
@@ -689,7 +686,7 @@ cudaError_t launch_attn_rows(const qtea_kv* kv, const AttnParams& base, cudaStre
   const int nt = rows <= 8 ? 1 : rows <= 16 ? 2 : 4;
   p.tile_tokens = 8 * nt / p.group;
   p.unit_shift = kv_unit_shift(kv->view.format);
-  p.item_cost = kv->view.format == QTEA_KV_F16 ? 16 : 8;
+  p.item_cost = kv->view.format == QTEA_KV_F16 ? 32 : 16;
   p.min_units = kv->view.format == QTEA_KV_F16 ? 24 : 12;
   if (!attn_cost_fits(p)) return cudaErrorInvalidValue;
   if (kv->view.format == QTEA_KV_F16) return launch_dim<QTEA_KV_F16>(kv, p, nt, st);

@@ -55,6 +55,29 @@ inline bool attn_cost_fits(const AttnParams& p) {
 
 #ifdef __CUDACC__
 
+// Launch with programmatic stream serialization: the grid may start while the kernel before it on the
+// stream drains, and waits for it (attn_begin) before it touches the caller's memory.
+template <class... Params, class... Args>
+cudaError_t attn_launch(void (*kernel)(Params...), int grid, int threads, int smem, cudaStream_t st, const Args&... args) {
+  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  if (e != cudaSuccess) return e;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(grid);
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
+__device__ __forceinline__ void attn_begin() {
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+}
+
 // One sequence of the batch.
 struct AttnSeq {
   int q0, n, base;  // first row, new tokens, position of the first

@@ -308,6 +308,7 @@ __global__ void __launch_bounds__((Chunk<FMT, D>::kThreads), 1)
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   const AttnTable tab = attn_table(smem_raw + T::kSmem, p.b.n_seqs);
+  attn_begin();
   attn_prefix(p, tab);  // ends with a barrier
   const AttnSplit split = attn_split(p, tab);
   if (split.total == 0 || (int)blockIdx.x >= split.ctas) return;
@@ -896,11 +897,8 @@ cudaError_t launch(const qtea_kv* kv, const ChunkParams& cp, const CUtensorMap& 
   using T = Chunk<FMT, D>;
   static_assert(T::kSmem + kAttnTableBytes(kKvMaxSeqs) + sizeof(ChunkShared) <= 227 * 1024, "shared memory of a CTA");
   const int smem = T::kSmem + kAttnTableBytes(cp.a.b.n_seqs);
-  auto k = qtea_attn_chunk_kernel<FMT, D>;
-  cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
-  if (e != cudaSuccess) return e;
-  k<<<std::min(kv->sm_count, kAttnMaxCtas), T::kThreads, smem, st>>>(kv->wide_k, kv->wide_v, map_q, cp);
-  return cudaGetLastError();
+  return attn_launch(qtea_attn_chunk_kernel<FMT, D>, std::min(kv->sm_count, kAttnMaxCtas), T::kThreads, smem, st,
+                     kv->wide_k, kv->wide_v, map_q, cp);
 }
 
 template <int FMT>
@@ -923,7 +921,7 @@ cudaError_t launch_attn_chunk(const qtea_kv* kv, const AttnParams& base, cudaStr
   cp.two = p.b.max_q > cp.half_tokens;
   p.tile_tokens = cp.two ? 2 * cp.half_tokens : cp.half_tokens;
   p.unit_shift = 7;
-  p.item_cost = 2;
+  p.item_cost = 5;  // about 5 us: 8 x 16 tokens 69, 62, 63, 63 us at 2, 4, 6, 12; two prompts 402, 387, 384, 392 us
   p.min_units = 3;
   if (!attn_cost_fits(p)) return cudaErrorInvalidValue;
   const bool negative = p.scale_log2 < 0.f;
