@@ -686,7 +686,10 @@ cudaError_t launch_attn_rows(const qtea_kv* kv, const AttnParams& base, cudaStre
   const int nt = rows <= 8 ? 1 : rows <= 16 ? 2 : 4;
   p.tile_tokens = 8 * nt / p.group;
   p.unit_shift = kv_unit_shift(kv->view.format);
-  p.item_cost = kv->view.format == QTEA_KV_F16 ? 32 : 16;
+  // What an item costs beside its units of about 8 KB (its page, queries, first copies, joins), and the
+  // least cost worth a CTA. 16 ragged sequences (fp8): 35, 33, 28, 29 us at 8, 16, 24, 32 units; one decode step (fp16):
+  // 12.0, 10.5, 10.0 us at 8, 16, 32, and 11.3, 13.5 us with 32, 48 as the least.
+  p.item_cost = kv->view.format == QTEA_KV_F16 ? 32 : kv->view.format == QTEA_KV_FP8 ? 24 : 16;
   p.min_units = kv->view.format == QTEA_KV_F16 ? 24 : 12;
   if (!attn_cost_fits(p)) return cudaErrorInvalidValue;
   if (kv->view.format == QTEA_KV_F16) return launch_dim<QTEA_KV_F16>(kv, p, nt, st);

@@ -828,31 +828,37 @@ __global__ void __launch_bounds__((Chunk<FMT, D>::kThreads), 1)
         if (live) store_lse(stat_of(m, l));
       } else {
         if (cp.two || g == 0) __stcg(slot + D * 256 + slot_row, stat_of(m, l));
-        __threadfence();
-        named_barrier<1>(256);
-        if (threadIdx.x == 0) {
-          const unsigned before = atomicAdd(p.counters + c0, 1u);
-          sh.is_last = before == (unsigned)(c1 - c0);
-          if (sh.is_last) p.counters[c0] = 0;
-        }
-        named_barrier<1>(256);
-        if (sh.is_last && live) {
-          __threadfence();
-          // four parts at a time, all of their loads in flight
-          const int parts = c1 - c0 + 1;
+        // As in the few-rows kernel: by eights in the place of the first of them, then those; four parts at a
+        // time with all of their loads in flight.
+        bool final = c1 - c0 < 8;
 #pragma unroll 1
-          for (int d = d0; d < d1; d += 16) {
+        for (bool joined = false;; final = joined = true) {  // joined: the eights have been
+          const int from = final ? c0 : c0 + (((int)blockIdx.x - c0) & ~7), step = joined ? 8 : 1;
+          const int n = joined ? (c1 - c0) / 8 + 1 : min(8, c1 - from + 1);
+          unsigned* counter = p.counters + (final ? 0 : from == c0 ? 1 : 2) * kAttnMaxCtas + from;
+          __threadfence();
+          named_barrier<1>(256);
+          if (threadIdx.x == 0) {
+            sh.is_last = atomicAdd(counter, 1u) == (unsigned)(n - 1);
+            if (sh.is_last) *counter = 0;  // ready for the next call
+          }
+          named_barrier<1>(256);
+          if (!sh.is_last) break;
+          __threadfence();
+          float stat = kNegInf;
+#pragma unroll 1
+          for (int d = live ? d0 : d1; d < d1; d += 16) {
             float v[16], top = kNegInf, total = 0.f;
 #pragma unroll
             for (int e = 0; e < 16; ++e) v[e] = 0.f;
 #pragma unroll 1
-            for (int i0 = 0; i0 < parts; i0 += 4) {
+            for (int i0 = 0; i0 < n; i0 += 4) {
               float st[4];
               float4 x[4][4];
 #pragma unroll
               for (int i = 0; i < 4; ++i) {
-                const float* part = slot_of(c0 + min(i0 + i, parts - 1));
-                st[i] = i0 + i < parts ? __ldcg(part + D * 256 + slot_row) : kNegInf;
+                const float* part = slot_of(from + step * min(i0 + i, n - 1));
+                st[i] = i0 + i < n ? __ldcg(part + D * 256 + slot_row) : kNegInf;
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
                   x[i][e] = __ldcg(reinterpret_cast<const float4*>(part) + (d / 4 + e) * 256 + slot_row);
@@ -867,7 +873,7 @@ __global__ void __launch_bounds__((Chunk<FMT, D>::kThreads), 1)
               for (int i = 0; i < 4; ++i) {
                 const float f = ex2(st[i] - ref);
                 total += f;
-                if (f != 0.f) {  // a part without keys for this row has not written it
+                if (f != 0.f) {  // a part without keys for this row may not have written it
 #pragma unroll
                   for (int e = 0; e < 4; ++e) {
                     v[4 * e] = fmaf(x[i][e].x, f, v[4 * e]), v[4 * e + 1] = fmaf(x[i][e].y, f, v[4 * e + 1]);
@@ -879,9 +885,22 @@ __global__ void __launch_bounds__((Chunk<FMT, D>::kThreads), 1)
             const float scale = total == 0.f ? 0.f : 1.f / total;
 #pragma unroll
             for (int e = 0; e < 16; ++e) v[e] *= scale;
-            store_row(d, v);
-            if (d == 0) store_lse(stat_of(top, total));
+            stat = stat_of(top, total);
+            if (final) {
+              store_row(d, v);
+            } else {  // only this thread reads here
+#pragma unroll
+              for (int e = 0; e < 16; e += 4)
+                __stcg(reinterpret_cast<float4*>(slot_of(from)) + ((d + e) / 4) * 256 + slot_row,
+                       make_float4(v[e], v[e + 1], v[e + 2], v[e + 3]));
+            }
           }
+          if (final) {
+            if (live) store_lse(stat);
+            break;
+          }
+          named_barrier<1>(256);  // the first part's stat has been read
+          if (cp.two || g == 0) __stcg(slot_of(from) + D * 256 + slot_row, stat);
         }
       }
     }
@@ -922,7 +941,7 @@ cudaError_t launch_attn_chunk(const qtea_kv* kv, const AttnParams& base, cudaStr
   p.tile_tokens = cp.two ? 2 * cp.half_tokens : cp.half_tokens;
   p.unit_shift = 7;
   p.item_cost = 5;  // about 5 us: 8 x 16 tokens 69, 62, 63, 63 us at 2, 4, 6, 12; two prompts 402, 387, 384, 392 us
-  p.min_units = 3;
+  p.min_units = 8;
   if (!attn_cost_fits(p)) return cudaErrorInvalidValue;
   const bool negative = p.scale_log2 < 0.f;
   cp.q_flip = negative ? 0x80008000u : 0u;
