@@ -58,14 +58,14 @@ __device__ __forceinline__ uint32_t transpose8(uint32_t a) {
   return r;
 }
 __device__ __forceinline__ void mma16816(float* c, const uint32_t* a, uint32_t b0, uint32_t b1) {
-  asm volatile(
+  asm(
       "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
       : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
       : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 // c = a * b
 __device__ __forceinline__ void mma16816_first(float* c, const uint32_t* a, uint32_t b0, uint32_t b1) {
-  asm volatile(
+  asm(
       "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
       "{%10, %10, %10, %10};"
       : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3])
@@ -100,6 +100,8 @@ struct Rows {
   static constexpr int kWide = kRowBytes < 128 ? kRowBytes : 128;  // bytes of a box's row
   static constexpr int kParts = kRowBytes / kWide;
   static constexpr int kSubs = kKeys / 16;  // a product takes 16 keys
+  // products' keys that go through the softmax together, as registers allow: two chains of work at a time
+  static constexpr int kTogether = FMT == QTEA_KV_F16 || NT == 4 ? 1 : 2;
   static constexpr int kBoxBytes = 16 * kWide;
   static constexpr int kSideBytes = kKeys * kRowBytes;
   static constexpr int kScaleRow = D / kKvBlock;
@@ -276,115 +278,70 @@ __global__ void __launch_bounds__(kWarps * 32, (Rows<FMT, D, NT>::kCtas))
       const uint32_t sbase = scales + stage * 2 * T::kScaleBytes;
       const int key_unit = (it.unit0 + warp + kWarps * i) << T::kShift;
       // 16 keys of the unit; `masked`: not every row of the tile sees all of them
-      auto step = [&](int sub, int key0, auto masked) {
-        constexpr bool kMasked = decltype(masked)::value;
-        const uint32_t kb = kbase + sub * T::kParts * T::kBoxBytes, vb = vbase + sub * T::kParts * T::kBoxBytes;
-        float s[NT][4];
-        {
-          if (FMT == QTEA_KV_F16) {
-            float odd[NT][4];  // every second product: half the chain
+      // S^T of 16 keys
+      auto scores = [&](int sub, float (*s)[4]) {
+        const uint32_t kb = kbase + sub * T::kParts * T::kBoxBytes;
+
+        if (FMT == QTEA_KV_F16) {
+          float odd[NT][4];  // every second product: half the chain
 #pragma unroll
-            for (int ks = 0; ks < KS; ++ks) {
-              const int x = 32 * ks;
-              uint32_t a[4];
-              ldmatrix4(a, kb + k_off[x % T::kWide / 32] + (x / T::kWide) * T::kBoxBytes);
+          for (int ks = 0; ks < KS; ++ks) {
+            const int x = 32 * ks;
+            uint32_t a[4];
+            ldmatrix4(a, kb + k_off[x % T::kWide / 32] + (x / T::kWide) * T::kBoxBytes);
 #pragma unroll
-              for (int nt = 0; nt < NT; ++nt) mma_q(ks & 1 ? odd[nt] : s[nt], a, ks, nt, ks < 2);
-            }
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-              for (int e = 0; e < 4; ++e) s[nt][e] += odd[nt][e];
-          } else {
-            // a block's codes are multiplied as they are, and its sum by the rows' powers of two
-            const uint32_t sk = sbase + sub * 16 * T::kScaleRow;
-            const uint32_t w0 = D == 128 ? lds32(sk + g * 4) : lds16(sk + g * 2);
-            const uint32_t w1 = D == 128 ? lds32(sk + (g + 8) * 4) : lds16(sk + (g + 8) * 2);
-            auto add_block = [&](int blk, const uint32_t* a0, const uint32_t* a1) {
-              const float f0 = scale_of(w0, blk), f1 = scale_of(w1, blk);
-#pragma unroll
-              for (int nt = 0; nt < NT; ++nt) {
-                float t[4];
-                mma_q(t, a0, 2 * blk, nt, true);
-                mma_q(t, a1, 2 * blk + 1, nt, false);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                  const float f = e < 2 ? f0 : f1;
-                  s[nt][e] = blk == 0 ? t[e] * f : fmaf(t[e], f, s[nt][e]);
-                }
-              }
-            };
-#pragma unroll
-            for (int x = 0; x < T::kRowBytes; x += 32) {
-              uint32_t r[4];
-              ldmatrix4(r, kb + k_off[x / 32]);
-              if (FMT == QTEA_KV_FP8) {
-                const uint32_t a0[4] = {from_e4m3x2(r[0]), from_e4m3x2(r[1]), from_e4m3x2_hi(r[0]), from_e4m3x2_hi(r[1])};
-                const uint32_t a1[4] = {from_e4m3x2(r[2]), from_e4m3x2(r[3]), from_e4m3x2_hi(r[2]), from_e4m3x2_hi(r[3])};
-                add_block(x / 32, a0, a1);
-              } else {
-#pragma unroll
-                for (int hb = 0; hb < 2; ++hb) {
-                  if (x / 16 + hb >= D / 32) break;
-                  uint32_t e0[4], e1[4];
-                  from_e2m1x8(r[2 * hb], e0);
-                  from_e2m1x8(r[2 * hb + 1], e1);
-                  const uint32_t a0[4] = {e0[0], e1[0], e0[1], e1[1]}, a1[4] = {e0[2], e1[2], e0[3], e1[3]};
-                  add_block(x / 16 + hb, a0, a1);
-                }
-              }
-            }
+            for (int nt = 0; nt < NT; ++nt) mma_q(ks & 1 ? odd[nt] : s[nt], a, ks, nt, ks < 2);
           }
-        }
-        // softmax weights
-        bool outrun = false;
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-          for (int col = 0; col < 2; ++col) {
-            const int h = kMasked ? seen(8 * nt + 2 * c + col) : 0, l = kMasked && p.window > 0 ? h - p.window : 0;
-#pragma unroll
-            for (int e = col; e < 4; e += 2) {
-              const int key = key0 + g + (e >> 1) * 8;
-              s[nt][e] = kMasked && (key < l || key >= h) ? kNegInf : s[nt][e] * p.scale_log2;
-              outrun |= s[nt][e] > m[nt][col] + kLag;
-            }
-          }
-        if (__any_sync(0xffffffffu, outrun)) {
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-              float top = fmaxf(s[nt][e], s[nt][e + 2]);
-              top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 4));
-              top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 8));
-              top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16));
-              const float next = fmaxf(m[nt][e], top);
-              const float f = next == kNegInf ? 1.f : ex2(m[nt][e] - next);
-              m[nt][e] = next;
-              l[nt][e] *= f;
+            for (int e = 0; e < 4; ++e) s[nt][e] += odd[nt][e];
+        } else {
+          // a block's codes are multiplied as they are, and its sum by the rows' powers of two
+          const uint32_t sk = sbase + sub * 16 * T::kScaleRow;
+          const uint32_t w0 = D == 128 ? lds32(sk + g * 4) : lds16(sk + g * 2);
+          const uint32_t w1 = D == 128 ? lds32(sk + (g + 8) * 4) : lds16(sk + (g + 8) * 2);
+          auto add_block = [&](int blk, const uint32_t* a0, const uint32_t* a1) {
+            const float f0 = scale_of(w0, blk), f1 = scale_of(w1, blk);
 #pragma unroll
-              for (int mt = 0; mt < MT; ++mt) o[mt][nt][e] *= f, o[mt][nt][e + 2] *= f;
+            for (int nt = 0; nt < NT; ++nt) {
+              float t[4];
+              mma_q(t, a0, 2 * blk, nt, true);
+              mma_q(t, a1, 2 * blk + 1, nt, false);
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                const float f = e < 2 ? f0 : f1;
+                s[nt][e] = blk == 0 ? t[e] * f : fmaf(t[e], f, s[nt][e]);
+              }
             }
-        }
-        uint32_t pf[NT][2];
+          };
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
+          for (int x = 0; x < T::kRowBytes; x += 32) {
+            uint32_t r[4];
+            ldmatrix4(r, kb + k_off[x / 32]);
+            if (FMT == QTEA_KV_FP8) {
+              const uint32_t a0[4] = {from_e4m3x2(r[0]), from_e4m3x2(r[1]), from_e4m3x2_hi(r[0]), from_e4m3x2_hi(r[1])};
+              const uint32_t a1[4] = {from_e4m3x2(r[2]), from_e4m3x2(r[3]), from_e4m3x2_hi(r[2]), from_e4m3x2_hi(r[3])};
+              add_block(x / 32, a0, a1);
+            } else {
 #pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            const float ref = m[nt][e] == kNegInf ? 0.f : m[nt][e];
-            s[nt][e] = ex2(s[nt][e] - ref);
-            s[nt][e + 2] = ex2(s[nt][e + 2] - ref);
-            l[nt][e] += s[nt][e] + s[nt][e + 2];
+              for (int hb = 0; hb < 2; ++hb) {
+                if (x / 16 + hb >= D / 32) break;
+                uint32_t e0[4], e1[4];
+                from_e2m1x8(r[2 * hb], e0);
+                from_e2m1x8(r[2 * hb + 1], e1);
+                const uint32_t a0[4] = {e0[0], e1[0], e0[1], e1[1]}, a1[4] = {e0[2], e1[2], e0[3], e1[3]};
+                add_block(x / 16 + hb, a0, a1);
+              }
+            }
           }
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            const __half2 w = __floats2half2_rn(s[nt][2 * h], s[nt][2 * h + 1]);
-            pf[nt][h] = transpose8(*reinterpret_cast<const uint32_t*>(&w));
-          }
         }
-        // O^T += V^T P^T. Where some keys lie outside all that the tile sees, their values and powers
-        // of two are replaced by zeros: 0 * NaN would reach the sums.
+            };
+      // O^T += V^T P^T over 16 keys. Where some keys lie outside all that the tile sees, their values and
+      // powers of two are replaced by zeros: 0 * NaN would reach the sums.
+      auto values = [&](int sub, int key0, const uint32_t (*pf)[2], auto masked) {
+        constexpr bool kMasked = decltype(masked)::value;
+        const uint32_t vb = vbase + sub * T::kParts * T::kBoxBytes;
         auto in = [&](int k) { return key0 + k >= lo_all && key0 + k < hi_all; };
         auto load_v = [&](uint32_t* r, uint32_t addr) {  // keys 2c, 2c+1 in r[0], r[1], 2c+8, 2c+9 in r[2], r[3]
           ldmatrix4_trans(r, addr);
@@ -450,11 +407,72 @@ __global__ void __launch_bounds__(kWarps * 32, (Rows<FMT, D, NT>::kCtas))
           }
         }
       };
+      // kTogether times 16 keys of the unit; `masked`: not every row of the tile sees all of them
+      auto step = [&](int sub, int key0, auto masked) {
+        constexpr bool kMasked = decltype(masked)::value;
+        float s[T::kTogether][NT][4];
+#pragma unroll
+        for (int u = 0; u < T::kTogether; ++u) scores(sub + u, s[u]);
+        bool outrun = false;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int col = 0; col < 2; ++col) {
+            const int h = kMasked ? seen(8 * nt + 2 * c + col) : 0, l = kMasked && p.window > 0 ? h - p.window : 0;
+#pragma unroll
+            for (int u = 0; u < T::kTogether; ++u)
+#pragma unroll
+              for (int e = col; e < 4; e += 2) {
+                const int key = key0 + 16 * u + g + (e >> 1) * 8;
+                s[u][nt][e] = kMasked && (key < l || key >= h) ? kNegInf : s[u][nt][e] * p.scale_log2;
+                outrun |= s[u][nt][e] > m[nt][col] + kLag;
+              }
+          }
+        if (__any_sync(0xffffffffu, outrun)) {
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              float top = kNegInf;
+#pragma unroll
+              for (int u = 0; u < T::kTogether; ++u) top = fmaxf(top, fmaxf(s[u][nt][e], s[u][nt][e + 2]));
+              top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 4));
+              top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 8));
+              top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16));
+              const float next = fmaxf(m[nt][e], top);
+              const float f = next == kNegInf ? 1.f : ex2(m[nt][e] - next);
+              m[nt][e] = next;
+              l[nt][e] *= f;
+#pragma unroll
+              for (int mt = 0; mt < MT; ++mt) o[mt][nt][e] *= f, o[mt][nt][e + 2] *= f;
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < T::kTogether; ++u) {
+          uint32_t pf[NT][2];
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              const float ref = m[nt][e] == kNegInf ? 0.f : m[nt][e];
+              s[u][nt][e] = ex2(s[u][nt][e] - ref);
+              s[u][nt][e + 2] = ex2(s[u][nt][e + 2] - ref);
+              l[nt][e] += s[u][nt][e] + s[u][nt][e + 2];
+            }
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              const __half2 w = __floats2half2_rn(s[u][nt][2 * h], s[u][nt][2 * h + 1]);
+              pf[nt][h] = transpose8(*reinterpret_cast<const uint32_t*>(&w));
+            }
+          }
+          values(sub + u, key0 + 16 * u, pf, masked);
+        }
+      };
 #pragma unroll 1
-      for (int sub = 0; sub < T::kSubs; ++sub) {
+      for (int sub = 0; sub < T::kSubs; sub += T::kTogether) {
         const int key0 = key_unit + 16 * sub;
-        if (key0 >= hi_all || key0 + 16 <= lo_all) continue;  // nothing of the tile sees these
-        if (key0 + 16 > hi_in || key0 < lo_in) step(sub, key0, std::true_type());
+        if (key0 >= hi_all || key0 + 16 * T::kTogether <= lo_all) continue;  // nothing of the tile sees these
+        if (key0 + 16 * T::kTogether > hi_in || key0 < lo_in) step(sub, key0, std::true_type());
         else step(sub, key0, std::false_type());
       }
       ++fills;
