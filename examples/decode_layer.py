@@ -1,0 +1,135 @@
+"""One decoder layer at decode time, every step but the activation on this library's kernels:
+
+    x = norm(h)                               qtea_norm
+    q, k, v = x Wq', x Wk', x Wv'             qtea_gemv_grouped (ternary weights, one launch)
+    k, v into the paged cache, q rotated      qtea_kv_append
+    a = attention over the cache              qtea_attention
+    h += a Wo',  x = norm(h)                  qtea_gemv, qtea_norm
+    g, u = x Wg', x Wu'                       qtea_gemv_grouped
+    h += (silu(g) u) Wd'                      torch, qtea_gemv, qtea_norm
+
+for a batch of sequences with one or a few new tokens each (16 in all at most, the GEMVs' largest
+batch), with random weights. `python examples/decode_layer.py --fmt fp8` prints the time of a step;
+with `--graph --seqs 1` the step is a captured graph (the GEMVs of two rows and more number their
+launches on the host, so a graph of those cannot be replayed).
+"""
+from __future__ import annotations
+
+import argparse
+import os
+import sys
+
+import numpy as np
+import torch
+
+sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
+
+import paper_2609_00224_gb300 as qt  # noqa: E402
+import synth  # noqa: E402
+
+FORMATS = {"f16": qt.QTEA_KV_F16, "fp8": qt.QTEA_KV_FP8, "fp4": qt.QTEA_KV_FP4}
+
+
+def _f16(a):
+    return torch.from_numpy(np.ascontiguousarray(a).view(np.int16)).cuda().view(torch.float16)
+
+
+class Linear:
+    """A ternary linear layer of N outputs and K inputs: its packed layout and operands."""
+
+    def __init__(self, N: int, K: int, seed: int):
+        p = self.problem = synth.make_problem("linear", N, K, 1, synth.salient_count(K), seed=seed)
+        self.layout = qt.qtea_pack_layout(torch.from_numpy(p.T).cuda(), n_salient=p.s)
+        self.operands = dict(layout=self.layout, row_scale=_f16(p.alpha.reshape(-1)), col_scale=_f16(p.v),
+                             salient_idx=torch.from_numpy(p.salient_idx).cuda(), residual_vals=_f16(p.residual_vals),
+                             residual_idx=torch.from_numpy(p.residual_idx).cuda())
+
+    def __call__(self, x):
+        return qt.qtea_gemv(x, **self.operands)
+
+
+class DecoderLayer:
+    def __init__(self, hidden=4096, q_heads=32, kv_heads=8, dim=128, inner=14336, fmt="fp8", page=64, max_seqs=16,
+                 max_context=8192, theta=500000.0, seed=1):
+        self.q_heads, self.dim, self.page = q_heads, dim, page
+        shapes = [(q_heads * dim, hidden), (kv_heads * dim, hidden), (kv_heads * dim, hidden), (hidden, q_heads * dim),
+                  (inner, hidden), (inner, hidden), (hidden, inner)]
+        self.wq, self.wk, self.wv, self.wo, self.wg, self.wu, self.wd = (
+            Linear(n, k, seed + i) for i, (n, k) in enumerate(shapes))
+        g = torch.Generator().manual_seed(seed)
+        self.norm_attn, self.norm_mlp = ((1 + 0.1 * torch.randn(hidden, generator=g)).half().cuda() for _ in range(2))
+        # random weights of these scales give large outputs: the residual takes a part of them
+        self.scale = 0.05
+        rate = theta ** (-torch.arange(dim // 2, dtype=torch.float64) / (dim // 2))
+        angle = torch.arange(max_context, dtype=torch.float64)[:, None] * rate
+        self.cos, self.sin = angle.cos().float().cuda(), angle.sin().float().cuda()
+        per_seq = -(-max_context // page)
+        self.cache = qt.KVCache.empty(max_seqs * per_seq, page, kv_heads, dim, fmt=FORMATS[fmt])
+        # each sequence's pages, strewn over the pool
+        self.pages = torch.randperm(max_seqs * per_seq, generator=g).view(max_seqs, per_seq).to(torch.int32).cuda()
+
+    def batch(self, q_len, ctx_len):
+        """The batch of sequences 0.. with these numbers of new tokens and lengths with them."""
+        starts = np.concatenate(([0], np.cumsum(q_len))).astype(np.int32)
+        return qt.KVBatch(torch.from_numpy(starts).cuda(), torch.tensor(ctx_len, dtype=torch.int32, device="cuda"),
+                          self.pages[:len(q_len)].contiguous(), n_tokens=int(starts[-1]), max_q_len=int(max(q_len)))
+
+    def step(self, h, batch):
+        """h: fp32 [tokens][hidden], the residual stream of the new tokens, updated in place."""
+        x = qt.qtea_norm(h, self.norm_attn)
+        q, k, v = qt.qtea_gemv_grouped([dict(x=x, **w.operands) for w in (self.wq, self.wk, self.wv)])
+        q = qt.qtea_kv_append(self.cache, batch, k, v, q=q, cos=self.cos, sin=self.sin)
+        a = qt.qtea_attention(self.cache, batch, q)
+        x = qt.qtea_norm(h, self.norm_mlp, y=self.wo(a.flatten(1)), res_scale=self.scale)
+        g, u = qt.qtea_gemv_grouped([dict(x=x, **w.operands) for w in (self.wg, self.wu)])
+        y = self.wd((torch.nn.functional.silu(g * self.scale) * u * self.scale).half())
+        qt.qtea_norm(h, y=y, res_scale=self.scale, want_x=False)
+        return h
+
+
+def main():
+    p = argparse.ArgumentParser(description=__doc__, formatter_class=argparse.RawDescriptionHelpFormatter)
+    p.add_argument("--fmt", choices=sorted(FORMATS), default="fp8")
+    p.add_argument("--seqs", type=int, default=4)
+    p.add_argument("--context", type=int, default=4000)
+    p.add_argument("--steps", type=int, default=20)
+    p.add_argument("--graph", action="store_true", help="capture the step in a CUDA graph and replay it (one sequence)")
+    a = p.parse_args()
+    if a.graph and a.seqs != 1:
+        p.error("--graph takes --seqs 1")
+    layer = DecoderLayer(fmt=a.fmt, max_seqs=a.seqs, max_context=a.context + a.steps + 8)
+    # what a prompt would have left in the cache
+    prompt = layer.batch([a.context] * a.seqs, [a.context] * a.seqs)
+    heads = layer.cache.n_kv_heads * layer.dim
+    k, v = (torch.randn(a.context * a.seqs, heads, device="cuda").half() for _ in range(2))
+    qt.qtea_kv_append(layer.cache, prompt, k, v)
+    batch = layer.batch([1] * a.seqs, [a.context + 1] * a.seqs)
+    h = torch.randn(a.seqs, 4096, device="cuda")
+    stream = torch.cuda.Stream()
+    with torch.cuda.stream(stream):
+        step = lambda: layer.step(h, batch)  # noqa: E731
+        step()
+        stream.synchronize()
+        if a.graph:
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph, stream=stream):
+                step()
+            step = graph.replay
+        for _ in range(3):
+            step()
+        begin, end = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+        begin.record()
+        for _ in range(a.steps):
+            step()
+            batch.ctx_len += 1  # on the device: a replayed step sees it
+        end.record()
+    torch.cuda.synchronize()
+    if qt.qtea_attention_status(qt.attention_workspace(stream=stream), stream=stream) != 0:
+        raise SystemExit("a kernel gave up a wait")
+    print(f"{a.seqs} sequences of {a.context} tokens, {a.fmt} cache: "
+          f"{begin.elapsed_time(end) / a.steps * 1e3:.1f} us per layer step"
+          f"{' (graph)' if a.graph else ''}, finite: {bool(torch.isfinite(h).all())}")
+
+
+if __name__ == "__main__":
+    main()

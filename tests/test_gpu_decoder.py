@@ -272,6 +272,47 @@ def test_attention_on_two_streams_with_their_own_workspaces(qt):
     assert all(torch.equal(a, b) for a, b in zip(outs, ref))
 
 
+def test_offsets_past_32_bits(qt):
+    """Pages more than 4 GB into the cache: written, read back and attended to as those at its start."""
+    n_pages, heads, dim, page = 20000, 8, 128, 128  # 5.2 GB a side
+    cache = qt.KVCache.empty(n_pages, page, heads, dim)
+    x = torch.randn(200, heads * dim, device="cuda").half()
+    q = torch.randn(1, 8, dim, device="cuda").half()
+    q40 = torch.randn(40, 8, dim, device="cuda").half()
+    got = []
+    for ids in ([3, 4], [n_pages - 1, n_pages - 2]):
+        make = lambda n: qt.KVBatch(torch.tensor([0, n], dtype=torch.int32, device="cuda"),  # noqa: E731
+                                    torch.tensor([200], dtype=torch.int32, device="cuda"),
+                                    torch.tensor([ids], dtype=torch.int32, device="cuda"), n, n)
+        qt.qtea_kv_append(cache, make(200), x, 2 * x)
+        k, v = qt.qtea_kv_read(cache, make(1), torch.tensor([0, 200], dtype=torch.int32, device="cuda"), n_rows=200)
+        assert torch.equal(k.flatten(1), x) and torch.equal(v.flatten(1), 2 * x)
+        got.append((qt.qtea_attention(cache, make(1), q), qt.qtea_attention(cache, make(40), q40)))
+    assert torch.equal(got[0][0], got[1][0]) and torch.equal(got[0][1], got[1][1])
+
+
+def test_status_reports_a_timeout_once_and_clears(qt):
+    n = qt.attention_workspace().numel()
+    ws = torch.zeros(n, dtype=torch.uint8, device="cuda")
+    ws.view(torch.int32)[0] = qt.QTEA_ERR_TIMEOUT  # as a kernel whose wait gave up would leave it
+    ws.view(torch.int32)[70] = 3
+    assert qt.qtea_attention_status(ws) == qt.QTEA_ERR_TIMEOUT
+    assert qt.qtea_attention_status(ws) == qt.QTEA_OK and not ws.any()
+
+
+def test_work_that_cannot_be_numbered_is_refused(qt):
+    import ctypes
+    from paper_2609_00224_gb300 import decoder as d
+    c = Case(qt, "f16", [1], [5], 4, 2, 64, 16, seed=22)
+    q, ws = torch.zeros(1, 4, 64, device="cuda").half(), qt.attention_workspace()
+    for n_seqs, max_pages, tokens, want in [(1, (1 << 27) - 1, 100, qt.QTEA_ERR_UNSUPPORTED), (513, 1, 1, qt.QTEA_ERR_INVALID_ARG),
+                                            (1, 1 << 27, 1, qt.QTEA_ERR_INVALID_ARG), (1, 0, 1, qt.QTEA_ERR_INVALID_ARG)]:
+        b = d._Batch(c.batch.q_start.data_ptr(), c.batch.ctx_len.data_ptr(), c.batch.pages.data_ptr(), n_seqs, max_pages,
+                     tokens, 1)
+        assert qt.load().qtea_attention(c.cache.handle, ctypes.byref(b), q.data_ptr(), 256, 4, 1.0, 0, q.data_ptr(), 256,
+                                        None, ws.data_ptr(), ws.numel(), None) == want
+
+
 # ------------------------------------------------------------------------------- cache: write and read
 
 
