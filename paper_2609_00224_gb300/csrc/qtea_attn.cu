@@ -3,23 +3,30 @@
 //
 // With R query rows sharing a cache head (tokens x query heads of the group, R <= 32) each cached
 // byte meets 2R multiply-adds at most: the kernel is bound by reading the cache, so its form
-// follows the copies. A warp works alone: it has its own ring of stages (8 KB of keys and values each at
-// head_dim 128), which its lanes refill with TMA boxes of 16 tokens, swizzled as the fragment loads
-// want them, and takes every fourth unit of the CTA's run. Nothing synchronises the CTA until its
+// follows the copies. A warp works alone: it has its own ring of stages (8 KB of keys and values each
+// at head_dim 128), which its lanes refill with TMA boxes swizzled as the fragment loads want
+// them, and takes every fourth unit of the CTA's run. Nothing synchronises the CTA until its
 // four warps' results are joined at the end of an item.
+//
+// GB300, device time: 32 decode steps over 4096 tokens each (fp16, 32 query heads on 8), 537 MB, 87 us
+// (6.2 TB/s); 16 ragged sequences (fp8, 40 on 8), 118 MB, 28 us; one over 131071 tokens (fp4, 64 on 8),
+// 143 MB, 41 us: there the conversions' pipe is half busy (153 of 302 warp instructions per 16 keys, two
+// clocks each), and 12 us are the first copies' latency and the joins; one over 517 tokens 10 us, nearly
+// all of it a chain of seven round trips to memory.
 //
 // Products run transposed on mma.sync m16n8k16: S^T = K Q^T with keys as the 16 rows and query rows as
 // the 8 columns, O^T = V^T P^T with head_dim as the rows. A group of 4 to 8 query heads then fills a
-// whole column tile, where queries as rows would leave 8 to 12 of 16 empty; an accumulator of O takes half the
-// registers; and softmax weights pass from S^T's layout to P^T's with two movmatrix per 16 keys.
+// whole column tile, where queries as rows would leave 8 to 12 of 16 empty; an accumulator of O
+// takes half the registers; and softmax weights pass from S^T's layout to P^T's with two movmatrix
+// per 16 keys.
 // The order of head_dim inside a product is free as long as both sides agree, so codes are used in
-// the order in which ldmatrix leaves them in a thread: E4M3 and E2M1 become fp16 by one conversion
-// per pair and one exact multiplication by their block's power of two.
+// the order in which ldmatrix leaves them in a thread. E4M3 and E2M1 become fp16 by one conversion
+// per pair; K's powers of two multiply the fp32 sums of their blocks, V's the fp16 values (exactly).
 //
 // The softmax runs in the base-2 domain against a reference that trails the running maximum by at
 // most kLag: weights are at most 2^kLag (fp16 holds them as precisely as those below 1), and the
 // accumulator is rescaled, and the row's maximum formed across lanes, only when the maximum
-// outruns the reference, a vote per 16 keys otherwise.
+// outruns the reference, a vote per 16 or 32 keys otherwise.
 #include <algorithm>
 #include <cstring>
 #include <type_traits>
@@ -59,7 +66,8 @@ __device__ __forceinline__ uint32_t transpose8(uint32_t a) {
 }
 __device__ __forceinline__ void mma16816(float* c, const uint32_t* a, uint32_t b0, uint32_t b1) {
   asm(
-      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
+      "{%0, %1, %2, %3};"
       : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
       : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
@@ -233,7 +241,7 @@ __global__ void __launch_bounds__(kWarps * 32, (Rows<FMT, D, NT>::kCtas))
     uint2 qf[kQShared ? 1 : KS][NT];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
-      const int r = 8 * nt + g, tok = it.seq.q0 + i0 + attn_token(p, r), h = it.head * p.group + r - attn_token(p, r) * p.group;
+      const int r = 8 * nt + g, t = attn_token(p, r), tok = it.seq.q0 + i0 + t, h = it.head * p.group + r - t * p.group;
       const __half* row = p.q + (long long)tok * p.q_ld + (long long)h * D;
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) {
@@ -705,8 +713,8 @@ cudaError_t launch_attn_rows(const qtea_kv* kv, const AttnParams& base, cudaStre
   p.tile_tokens = 8 * nt / p.group;
   p.unit_shift = kv_unit_shift(kv->view.format);
   // What an item costs beside its units of about 8 KB (its page, queries, first copies, joins), and the
-  // least cost worth a CTA. 16 ragged sequences (fp8): 35, 33, 28, 29 us at 8, 16, 24, 32 units; one decode step (fp16):
-  // 12.0, 10.5, 10.0 us at 8, 16, 32, and 11.3, 13.5 us with 32, 48 as the least.
+  // least cost worth a CTA. 16 ragged sequences (fp8): 35, 33, 28, 29 us at 8, 16, 24, 32 units; one
+  // decode step (fp16): 12.0, 10.5, 10.0 us at 8, 16, 32, and 11.3, 13.5 us with 32, 48 as the least.
   p.item_cost = kv->view.format == QTEA_KV_F16 ? 32 : kv->view.format == QTEA_KV_FP8 ? 24 : 16;
   p.min_units = kv->view.format == QTEA_KV_F16 ? 24 : 12;
   if (!attn_cost_fits(p)) return cudaErrorInvalidValue;

@@ -58,7 +58,8 @@ inline bool attn_cost_fits(const AttnParams& p) {
 // Launch with programmatic stream serialization: the grid may start while the kernel before it on the
 // stream drains, and waits for it (attn_begin) before it touches the caller's memory.
 template <class... Params, class... Args>
-cudaError_t attn_launch(void (*kernel)(Params...), int grid, int threads, int smem, cudaStream_t st, const Args&... args) {
+cudaError_t attn_launch(void (*kernel)(Params...), int grid, int threads, int smem, cudaStream_t st,
+                        const Args&... args) {
   cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   if (e != cudaSuccess) return e;
   cudaLaunchAttribute attr[1];
@@ -106,7 +107,9 @@ __device__ __forceinline__ AttnSeq attn_seq(const AttnParams& p, int s) {
 }
 
 // r / group for a row of a tile: exact for r < 256 and group <= 32.
-__device__ __forceinline__ int attn_token(const AttnParams& p, int r) { return (int)((unsigned)r * p.group_inverse >> 16); }
+__device__ __forceinline__ int attn_token(const AttnParams& p, int r) {
+  return (int)((unsigned)r * p.group_inverse >> 16);
+}
 
 // The units of tile t of a sequence: first unit and their number (at least one, for tiles that see
 // nothing have zeros to write).

@@ -12,16 +12,21 @@
 //  * the weights go back to TMEM over S, as fp16, and are the second product's A operand from there;
 //  * over an fp16 cache, a row's weights are formed against the reference that it has, its maximum in
 //    the first unit, without looking for this unit's maximum first: that is known when the weights
-//    are, and only where a weight passes 2^15, near fp16's end, are they formed again against a new reference
-//    and the accumulator rescaled. Until then a thread holds 64 registers of weights; over a
-//    quantised cache the converting warps need those registers, so there the maximum is looked for
+//    are, and only where a weight passes 2^15, near fp16's end, are they formed again against a new
+//    reference and the accumulator rescaled. Until then a thread holds 64 registers of weights; over
+//    a quantised cache the converting warps need those registers, so there the maximum is looked for
 //    first, in a second reading of S, and the reference follows it by at most 2^8;
-//  * one warp issues every product, one warp every copy; keys and values are boxes of a page,
+//  * one warp issues every product, two warps the copies; keys and values are boxes of a page,
 //    swizzled on the way into shared memory. K is the second operand K-major, V is taken MN-major, so
 //    neither is transposed. Quantised rows are copied as they are into a ring of their own, and four
 //    warps write them as fp16 (exactly) in the same swizzled form.
 // The tensor pipe executes one thread's products in order, which replaces most barriers: when S of
 // step j+1 has been signalled, O of step j is complete and its weights' columns are free.
+//
+// GB300, device time: chunks of 2048 and 1000 tokens over 16384 and 5001 (fp16, 32 query heads on 8), 589
+// GFLOP, 386 us (1.53 PFLOP/s, tensor pipe 66 % busy: S's products read both operands from shared memory at
+// its full rate, which the copies share); 8 sequences of 16 tokens over 11 k (fp8, 64 on 8), 190 MB, 65 us:
+// one row tile leaves a chain of conversion, product, softmax, product that two groups do not cover.
 #include <cudaTypedefs.h>
 
 #include <algorithm>
@@ -79,8 +84,10 @@ __device__ __forceinline__ void tmem_fence_after() { asm volatile("tcgen05.fence
 __device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
-#define QTEA_R8(r, i) "=r"(r[i]), "=r"(r[i + 1]), "=r"(r[i + 2]), "=r"(r[i + 3]), "=r"(r[i + 4]), "=r"(r[i + 5]), "=r"(r[i + 6]), "=r"(r[i + 7])
-#define QTEA_W8(r, i) "r"(r[i]), "r"(r[i + 1]), "r"(r[i + 2]), "r"(r[i + 3]), "r"(r[i + 4]), "r"(r[i + 5]), "r"(r[i + 6]), "r"(r[i + 7])
+#define QTEA_R4(r, i) "=r"(r[i]), "=r"(r[i + 1]), "=r"(r[i + 2]), "=r"(r[i + 3])
+#define QTEA_W4(r, i) "r"(r[i]), "r"(r[i + 1]), "r"(r[i + 2]), "r"(r[i + 3])
+#define QTEA_R8(r, i) QTEA_R4(r, i), QTEA_R4(r, i + 4)
+#define QTEA_W8(r, i) QTEA_W4(r, i), QTEA_W4(r, i + 4)
 
 // 32 consecutive columns of this thread's lane
 __device__ __forceinline__ void tmem_ld32(uint32_t* r, uint32_t addr) {
@@ -117,8 +124,8 @@ __device__ __forceinline__ void tmem_st16(uint32_t addr, const uint32_t* r) {
 
 __device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar) {
   asm volatile(
-      "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::
-          "r"(dst),
+      "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
+      " [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst),
       "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(bar)
       : "memory");
 }
@@ -132,7 +139,10 @@ __device__ __forceinline__ void sts128(uint32_t a, uint4 v) {
 }
 __device__ __forceinline__ uint4 lds128(uint32_t a) {
   uint4 v;
-  asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a) : "memory");
+  asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
+               : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
+               : "r"(a)
+               : "memory");
   return v;
 }
 __device__ __forceinline__ uint32_t lds32(uint32_t a) {
@@ -384,7 +394,8 @@ __global__ void __launch_bounds__((Chunk<FMT, D>::kThreads), 1)
       constexpr uint32_t kIdescO = 1u << 4 | 1u << 16 | (D >> 3) << 17 | (kRowsTile >> 4) << 24;
       uint32_t stage = 0, phase = 0;
       uint32_t q_phase = 0, o_phase = 1, p_phase[2] = {0, 0};
-      const uint64_t q_desc = operand(q_smem, 16), k_desc = operand(kv_smem, 16), v_desc = operand(kv_smem, T::kPartBytes);
+      const uint64_t q_desc = operand(q_smem, 16), k_desc = operand(kv_smem, 16);
+      const uint64_t v_desc = operand(kv_smem, T::kPartBytes);
       for (int cur = begin; cur < end;) {
         const AttnItem it = attn_item(p, tab, cur, end);
         cur = it.next;
@@ -619,7 +630,6 @@ __global__ void __launch_bounds__((Chunk<FMT, D>::kThreads), 1)
     }
   } else {
     // ---------------------------------------------------------------------------------- softmax
-    
     const int g = warp >> 2, row = threadIdx.x & 127;
     const uint32_t lanes = tmem + ((uint32_t)(warp & 3) << 21);  // this warp's 32 lanes
     const uint32_t s_addr = lanes + g * 128, o_addr = lanes + 256 + g * 128;
@@ -719,7 +729,8 @@ __global__ void __launch_bounds__((Chunk<FMT, D>::kThreads), 1)
         } else {
           uint32_t w[kUnit / 2];
           // a reference is wanted in the first unit that a row sees something of
-          if (__any_sync(0xffffffffu, live && m == kNegInf && key0 < hi && (p.window == 0 || key0 + kUnit > hi - p.window))) refer(0.f);
+          const bool sees = key0 < hi && (p.window == 0 || key0 + kUnit > hi - p.window);
+          if (__any_sync(0xffffffffu, live && m == kNegInf && sees)) refer(0.f);
           for (;;) {
             sum[0] = sum[1] = make_float2(0.f, 0.f);
             over[0] = over[1] = kNegInf;
@@ -770,7 +781,7 @@ __global__ void __launch_bounds__((Chunk<FMT, D>::kThreads), 1)
       const float inv = l == 0.f ? 0.f : 1.f / l;
       fa *= inv, fb *= inv;
       const bool some = cp.two ? steps > 0 : true;  // whether there are accumulators to read
-      const int tok = it.seq.q0 + t0 + attn_token(p, row), head = it.head * p.group + (row - attn_token(p, row) * p.group);
+      const int t = attn_token(p, row), tok = it.seq.q0 + t0 + t, head = it.head * p.group + row - t * p.group;
       // a partial result: O / l as [D/4][256][4], then m + log2 l
       constexpr size_t kSlot = (size_t)2 * kRowsTile * (128 + 1);
       auto slot_of = [&](int cta) { return p.slots + (2 * (size_t)cta + (cta == c0 ? 1 : 0)) * kSlot; };
@@ -940,7 +951,9 @@ cudaError_t launch_attn_chunk(const qtea_kv* kv, const AttnParams& base, cudaStr
   cp.two = p.b.max_q > cp.half_tokens;
   p.tile_tokens = cp.two ? 2 * cp.half_tokens : cp.half_tokens;
   p.unit_shift = 7;
-  p.item_cost = 5;  // about 5 us: 8 x 16 tokens 69, 62, 63, 63 us at 2, 4, 6, 12; two prompts 402, 387, 384, 392 us
+  // an item costs about 5 us beside its units: 8 x 16 tokens took 69, 62, 63, 63 us with 2, 4, 6, 12 here, two
+  // prompts 402, 387, 384, 392 us; 16 tokens over 131072 took 94, 87, 93 us with 3, 8, 12 as the least
+  p.item_cost = 5;
   p.min_units = 8;
   if (!attn_cost_fits(p)) return cudaErrorInvalidValue;
   const bool negative = p.scale_log2 < 0.f;

@@ -51,7 +51,8 @@ __device__ __forceinline__ int kv_context(const KvBatchView& b, const KvView& kv
 struct KvFound {
   int s, first, next, ctx;
 };
-__device__ __forceinline__ KvFound kv_find_sequence(const int32_t* start, const KvBatchView& b, const KvView& kv, int row) {
+__device__ __forceinline__ KvFound kv_find_sequence(const int32_t* start, const KvBatchView& b, const KvView& kv,
+                                                    int row) {
   const int lane = threadIdx.x & 31;
   KvFound f{-1, 0, 0, 0};
   for (int base = 0; base < b.n_seqs; base += 32) {
@@ -138,7 +139,9 @@ __device__ __forceinline__ uint32_t scale_high(uint32_t w) { return ((w & 0x1f1f
 // of the selected byte's top bit: zeros.
 __device__ __forceinline__ uint32_t scale_pair(uint32_t h0, uint32_t h1, int blk) {
   uint32_t r;
-  asm("prmt.b32 %0, %1, %2, %3;" : "=r"(r) : "r"(h0), "r"(h1), "r"((8 | blk) | blk << 4 | (12 | blk) << 8 | (4 | blk) << 12));
+  asm("prmt.b32 %0, %1, %2, %3;"
+      : "=r"(r)
+      : "r"(h0), "r"(h1), "r"((8 | blk) | blk << 4 | (12 | blk) << 8 | (4 | blk) << 12));
   return r;
 }
 #endif

@@ -200,9 +200,9 @@ __global__ void __launch_bounds__(C == 1 ? 1024 : 512, C == 1 && VEC ? 2 : 1) qt
   }
 }
 
-// Rows longer than the registers hold, and those past 8192 columns without 16-byte accesses: the row is read again from memory after each sum. h' goes to
-// h_out, and is formed a second time (from h and y, which h_out may overwrite: each thread reads and
-// writes its own elements only) for x.
+// Rows longer than the registers hold, and those past 8192 columns without 16-byte accesses: the row
+// is read again from memory after each sum. h' goes to h_out, and is formed a second time (from h and
+// y, which h_out may overwrite: each thread reads and writes its own elements only) for x.
 template <int HT, int YT>
 __global__ void __launch_bounds__(1024) qtea_norm_long_kernel(const NormParams p) {
   __shared__ float part[2][32];
@@ -256,7 +256,7 @@ template <int HT, int YT>
 void launch_types(const NormParams& p, bool vec, cudaStream_t st) {
   const int grid = std::min(p.n_rows, 1 << 20);
   const int per8 = (p.n + 7) / 8;  // chunks of eight in a row
-  const bool wide = per8 > 1024;   // more than a chunk for each of the most threads
+  const bool wide = per8 > 1024;  // more than a chunk for each of the most threads
   const int threads = std::max(32, (((wide ? (per8 + 3) / 4 : per8) + 31) / 32) * 32);
   if (wide && (!vec || per8 > 4 * 512)) {
     qtea_norm_long_kernel<HT, YT><<<grid, 1024, 0, st>>>(p);
@@ -287,7 +287,8 @@ extern "C" int qtea_norm(const qtea_norm_args* a, qtea_stream_t stream) {
   const long long n = a->n_cols;
   const int hs = size(a->h_type), ys = size(a->y_type);
   if (!a->h || a->h_ld < n || !multiple(a->h, 0, 1, hs)) return QTEA_ERR_INVALID_ARG;
-  if (a->y && (a->y_ld < n || !multiple(a->y, 0, 1, ys) || !a->h_out || a->h_out_ld < n || !multiple(a->h_out, 0, 1, hs)))
+  if (a->y && (a->y_ld < n || !multiple(a->y, 0, 1, ys))) return QTEA_ERR_INVALID_ARG;
+  if (a->y && (!a->h_out || a->h_out_ld < n || !multiple(a->h_out, 0, 1, hs)))
     return QTEA_ERR_INVALID_ARG;
   if (!a->y && (!a->x || a->post_weight || a->gate)) return QTEA_ERR_INVALID_ARG;
   if (a->x && (!a->weight || a->x_ld < n)) return QTEA_ERR_INVALID_ARG;

@@ -379,7 +379,8 @@ def qtea_norm(h, weight=None, y=None, post_weight=None, gate=None, res_scale: fl
         raise ValueError("nothing to do without y and x")
     else:
         x = None
-    args = _NORM.pack(hp, yp, pw, gp, wp, hop, xp, h_ld, y_ld, g_ld, ho_ld, x_ld, h_type, y_type, n, cols, res_scale, eps)
+    args = _NORM.pack(hp, yp, pw, gp, wp, hop, xp, h_ld, y_ld, g_ld, ho_ld, x_ld, h_type, y_type, n, cols, res_scale,
+                      eps)
     rc = lib.qtea_norm(args, _stream_of(stream, h.get_device()))
     if rc:
         _fail(rc, "qtea_norm")
