@@ -1,7 +1,7 @@
 // Attention of a few query rows per cache head over the paged cache (decode steps, drafted tokens),
 // and the entry points of qtea_attention.
 //
-// With R query rows sharing a cache head (tokens x query heads of the group, R <= 32) each cached
+// With R query rows sharing a cache head (tokens x query heads of the group, R <= 16) each cached
 // byte meets 2R multiply-adds at most: the kernel is bound by reading the cache, so its form
 // follows the copies. A warp works alone: it has its own ring of stages (8 KB of keys and values each
 // at head_dim 128), which its lanes refill with TMA boxes swizzled as the fragment loads want
@@ -37,7 +37,7 @@ namespace qtea {
 namespace {
 
 constexpr int kWarps = 4;
-constexpr int kMaxRows = 32;
+constexpr int kMaxRows = 16;  // query rows of a cache head: two column tiles
 constexpr float kLag = 8.f;
 constexpr float kNegInf = -INFINITY;
 
@@ -79,6 +79,10 @@ __device__ __forceinline__ void mma16816_first(float* c, const uint32_t* a, uint
       : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3])
       : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
 }
+__device__ __forceinline__ void mma_q(float* c, const uint32_t* a, uint2 b, bool first) {
+  if (first) mma16816_first(c, a, b.x, b.y);
+  else mma16816(c, a, b.x, b.y);
+}
 __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
   asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst),
                "l"(reinterpret_cast<uint64_t>(src)), "r"(bytes), "r"(bar)
@@ -108,8 +112,8 @@ struct Rows {
   static constexpr int kWide = kRowBytes < 128 ? kRowBytes : 128;  // bytes of a box's row
   static constexpr int kParts = kRowBytes / kWide;
   static constexpr int kSubs = kKeys / 16;  // a product takes 16 keys
-  // products' keys that go through the softmax together, as registers allow: two chains of work at a time
-  static constexpr int kTogether = FMT == QTEA_KV_F16 || NT == 4 ? 1 : 2;
+  // products' keys that go through the softmax together: two chains of work at a time (an fp16 unit is one)
+  static constexpr int kTogether = FMT == QTEA_KV_F16 ? 1 : 2;
   static constexpr int kBoxBytes = 16 * kWide;
   static constexpr int kSideBytes = kKeys * kRowBytes;
   static constexpr int kScaleRow = D / kKvBlock;
@@ -142,10 +146,6 @@ __global__ void __launch_bounds__(kWarps * 32, (Rows<FMT, D, NT>::kCtas))
   __shared__ float stat_m[kWarps][R], stat_l[kWarps][R], joined_m[R], joined_l[R];
   __shared__ int is_last;
   __shared__ int span[3], end;
-  // Q^T fragments of four column tiles do not fit the registers beside O^T: they are read from here
-  constexpr bool kQShared = NT == 4;
-  __shared__ uint2 q_shared[kQShared ? KS * NT * 32 : 1];
-
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, c = lane & 3;
   if (lane == 0) {
 #pragma unroll
@@ -238,33 +238,24 @@ __global__ void __launch_bounds__(kWarps * 32, (Rows<FMT, D, NT>::kCtas))
     auto seen = [&](int r) { return r < rows ? it.seq.base + i0 + attn_token(p, r) + 1 : 0; };
 
     // Q^T fragments: column (query row) 8 nt + g, head_dim in the order of the format's codes.
-    uint2 qf[kQShared ? 1 : KS][NT];
+    uint2 qf[KS][NT];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
       const int r = 8 * nt + g, t = attn_token(p, r), tok = it.seq.q0 + i0 + t, h = it.head * p.group + r - t * p.group;
       const __half* row = p.q + (long long)tok * p.q_ld + (long long)h * D;
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) {
-        if (kQShared && ks % kWarps != warp) continue;  // the warps share the loads
         const int d0 = FMT == QTEA_KV_F16   ? 16 * ks + 2 * c
                        : FMT == QTEA_KV_FP8 ? 16 * ks + 4 * c
                                             : 32 * (ks >> 1) + 8 * c + 4 * (ks & 1);
         const int d1 = d0 + (FMT == QTEA_KV_F16 ? 8 : 2);
-        uint2 v = make_uint2(0u, 0u);
+        qf[ks][nt] = make_uint2(0u, 0u);
         if (r < rows) {
-          v.x = *reinterpret_cast<const uint32_t*>(row + d0);
-          v.y = *reinterpret_cast<const uint32_t*>(row + d1);
+          qf[ks][nt].x = *reinterpret_cast<const uint32_t*>(row + d0);
+          qf[ks][nt].y = *reinterpret_cast<const uint32_t*>(row + d1);
         }
-        if (kQShared) q_shared[(ks * NT + nt) * 32 + lane] = v;
-        else qf[kQShared ? 0 : ks][nt] = v;
       }
     }
-    if (kQShared) __syncthreads();
-    auto mma_q = [&](float* acc, const uint32_t* a, int ks, int nt, bool first) {
-      const uint2 b = kQShared ? q_shared[(ks * NT + nt) * 32 + lane] : qf[kQShared ? 0 : ks][nt];
-      if (first) mma16816_first(acc, a, b.x, b.y);
-      else mma16816(acc, a, b.x, b.y);
-    };
 
     float o[MT][NT][4];
     // the reference (-infinity while nothing has been seen), and this thread's sums
@@ -298,7 +289,7 @@ __global__ void __launch_bounds__(kWarps * 32, (Rows<FMT, D, NT>::kCtas))
             uint32_t a[4];
             ldmatrix4(a, kb + k_off[x % T::kWide / 32] + (x / T::kWide) * T::kBoxBytes);
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) mma_q(ks & 1 ? odd[nt] : s[nt], a, ks, nt, ks < 2);
+            for (int nt = 0; nt < NT; ++nt) mma_q(ks & 1 ? odd[nt] : s[nt], a, qf[ks][nt], ks < 2);
           }
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt)
@@ -314,8 +305,8 @@ __global__ void __launch_bounds__(kWarps * 32, (Rows<FMT, D, NT>::kCtas))
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
               float t[4];
-              mma_q(t, a0, 2 * blk, nt, true);
-              mma_q(t, a1, 2 * blk + 1, nt, false);
+              mma_q(t, a0, qf[2 * blk][nt], true);
+              mma_q(t, a1, qf[2 * blk + 1][nt], false);
 #pragma unroll
               for (int e = 0; e < 4; ++e) {
                 const float f = e < 2 ? f0 : f1;
@@ -689,9 +680,7 @@ cudaError_t launch(const qtea_kv* kv, const AttnParams& p, cudaStream_t st) {
 
 template <int FMT, int D>
 cudaError_t launch_nt(const qtea_kv* kv, const AttnParams& p, int nt, cudaStream_t st) {
-  if (nt == 1) return launch<FMT, D, 1>(kv, p, st);
-  if (nt == 2) return launch<FMT, D, 2>(kv, p, st);
-  return launch<FMT, D, 4>(kv, p, st);
+  return nt == 1 ? launch<FMT, D, 1>(kv, p, st) : launch<FMT, D, 2>(kv, p, st);
 }
 
 template <int FMT>
@@ -701,15 +690,13 @@ cudaError_t launch_dim(const qtea_kv* kv, const AttnParams& p, int nt, cudaStrea
 
 }  // namespace
 
-size_t attn_rows_floats(int sm_count) {  // two CTAs of 32 rows an SM, or three of 8
-  return (size_t)2 * sm_count * (128 * kMaxRows + 2 * kMaxRows);
+size_t attn_rows_floats(int sm_count) {  // two CTAs of 16 rows an SM, or three of 8
+  return (size_t)2 * sm_count * (128 * kMaxRows + kMaxRows);
 }
 
 cudaError_t launch_attn_rows(const qtea_kv* kv, const AttnParams& base, cudaStream_t st) {
   AttnParams p = base;
-  // column tiles of 8 rows: the fewest that hold the longest sequence's rows, or whole tokens at 32
-  const long long rows = (long long)p.group * p.b.max_q;
-  const int nt = rows <= 8 ? 1 : rows <= 16 ? 2 : 4;
+  const int nt = p.group * p.b.max_q <= 8 ? 1 : 2;  // column tiles of 8 rows
   p.tile_tokens = 8 * nt / p.group;
   p.unit_shift = kv_unit_shift(kv->view.format);
   // What an item costs beside its units of about 8 KB (its page, queries, first copies, joins), and the
@@ -780,6 +767,9 @@ int qtea_attention(const qtea_kv* kv, const qtea_kv_batch* batch, const uint16_t
   p.counters = reinterpret_cast<unsigned*>(workspace) + 64;
   p.slots = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + kAttnHeaderBytes);
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+  // 32 rows took this kernel (four column tiles, their queries in shared memory) 67, 58, 58 us for 8
+  // sequences of 8192 tokens in fp16, fp8, fp4 at head_dim 128, and the many-rows kernel 55, 49, 43; 16
+  // rows 53, 36, 35 against 56, 49, 43.
   const bool few = (long long)p.group * p.b.max_q <= kMaxRows;
   const cudaError_t e = few ? launch_attn_rows(kv, p, st) : launch_attn_chunk(kv, p, st);
   if (e == cudaErrorInvalidValue) return QTEA_ERR_UNSUPPORTED;
