@@ -271,11 +271,17 @@ def qtea_kv_read(cache: KVCache, batch: KVBatch, row_start, n_rows=None, k_out=N
 
 
 _workspaces = {}
+_WORKSPACE_HEADER = 16384  # bytes ahead of the partial results (kAttnHeaderBytes in csrc/qtea_attn.h)
 
 
 def attention_workspace(device=None, stream=None):
     """The workspace that qtea_attention uses on a stream when it is given none (one per device and
-    stream, zeroed when it is made and kept: calls on one stream are in order)."""
+    stream, zeroed when it is made and kept: calls on one stream are in order).
+
+    While the stream is captured a new one is not kept: it lies in the graph's memory, and its counters
+    are zeroed by the graph itself, at every replay. A graph that should not carry that has its
+    stream's workspace made before the capture.
+    """
     import torch
     lib = _lib()
     device = torch.cuda.current_device() if device is None else device
@@ -283,14 +289,15 @@ def attention_workspace(device=None, stream=None):
     ws = _workspaces.get((device, raw))
     if ws is None:
         n = ctypes.c_size_t()
-        with torch.cuda.device(device):
+        on = torch.cuda.ExternalStream(raw, device=device) if raw else torch.cuda.default_stream(device)
+        with torch.cuda.device(device), torch.cuda.stream(on):
             rc = lib.qtea_attention_workspace(ctypes.byref(n))
             if rc:
                 _fail(rc, "qtea_attention_workspace")
-            ws = torch.zeros(n.value, dtype=torch.uint8, device=f"cuda:{device}")
+            ws = torch.empty(n.value, dtype=torch.uint8, device=f"cuda:{device}")
+            ws[:_WORKSPACE_HEADER].zero_()  # the status and the counters; partial results need no zeros
             if not torch.cuda.is_current_stream_capturing():
-                torch.cuda.current_stream().synchronize()  # the call may be for another stream
-        _workspaces[(device, raw)] = ws
+                _workspaces[(device, raw)] = ws
     return ws
 
 

@@ -50,3 +50,10 @@ def test_norm_refusals():
                dict(gate_ld=63), dict(gate=257), dict(post_weight=257), dict(h_type=2), dict(y_type=-1),
                dict(y=None), dict(y=None, post_weight=None, gate=None, x=None)):
         assert norm(**kw) == BAD, kw
+
+
+def test_workspace_header_is_the_kernels():
+    import pathlib
+    import re
+    text = (pathlib.Path(qt.__file__).parent / "csrc" / "qtea_attn.h").read_text()
+    assert int(re.search(r"kAttnHeaderBytes = (\d+);", text).group(1)) == d._WORKSPACE_HEADER

@@ -256,6 +256,42 @@ def test_attention_replays_in_a_graph_with_other_lengths(qt):
         assert torch.equal(out, qt.qtea_attention(c.cache, c.batch, q))
 
 
+def test_attention_captured_on_a_stream_without_a_workspace(qt):
+    """The first call of a stream under capture: no graph's workspace waits for another graph's replay."""
+    c = Case(qt, "f16", [1, 1], [4000, 900], 8, 2, 128, 32, seed=8)
+    q = torch.randn(2, 8, 128, device="cuda").half()
+    ref = qt.qtea_attention(c.cache, c.batch, q)
+    s = torch.cuda.Stream()
+    outs, graphs = [torch.zeros_like(q) for _ in range(3)], []
+    for out in outs[:2]:
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=s):
+            qt.qtea_attention(c.cache, c.batch, q, out=out)
+            qt.qtea_attention(c.cache, c.batch, q, out=out)
+        graphs.append(g)
+    with torch.cuda.stream(s):
+        qt.qtea_attention(c.cache, c.batch, q, out=outs[2])
+    torch.cuda.synchronize()
+    for g in reversed(graphs):
+        g.replay()
+        g.replay()
+        torch.cuda.synchronize()
+    assert all(torch.equal(out, ref) for out in outs)
+
+
+@pytest.mark.parametrize("fmt", list(FMTS))
+@pytest.mark.parametrize("rows", [1, 40, 150])
+def test_attention_reads_no_partial_result_that_it_did_not_write(qt, fmt, rows):
+    """Only the workspace's counters start as zeros: NaN in all the rest changes nothing."""
+    c = Case(qt, fmt, [rows, 1], [3000, 700], 8, 2, 128, 64, seed=11)
+    q = torch.randn(c.tokens, 8, 128, device="cuda").half()
+    ws = torch.full((qt.attention_workspace().numel(),), 255, dtype=torch.uint8, device="cuda")
+    ws[:16384] = 0
+    ref = qt.qtea_attention(c.cache, c.batch, q)
+    assert torch.isfinite(ref).all()
+    assert torch.equal(qt.qtea_attention(c.cache, c.batch, q, workspace=ws), ref)
+
+
 def test_attention_on_two_streams_with_their_own_workspaces(qt):
     c = Case(qt, "f16", [1, 1], [4000, 900], 8, 2, 128, 32, seed=7)
     q = [torch.randn(2, 8, 128, device="cuda").half() for _ in range(2)]
