@@ -4,6 +4,9 @@ attention over it, and the norms around a block (the second part of ``include/qt
 The functions have the C entry points' names. They sit in a decode loop where a call takes a few
 microseconds, so what does not change between calls is checked and laid out once, in a ``KVCache``
 and a ``KVBatch``; a call then checks its own tensors only.
+
+A call runs on `stream` (the current one by default). Outputs that it makes come from that stream's
+memory; tensors of another stream's that are given to it are the caller's to keep until it has run.
 """
 from __future__ import annotations
 
@@ -73,6 +76,24 @@ def _stream_of(stream, device):
     if stream is None:
         return _state["raw_stream"](device)
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
+
+
+def _on(stream, device):
+    """The torch stream of a stream or handle."""
+    import torch
+    if hasattr(stream, "cuda_stream"):
+        return stream
+    return torch.cuda.ExternalStream(stream, device=device) if stream else torch.cuda.default_stream(device)
+
+
+def _new(shape, dtype, device, stream):
+    """An output of a call on `stream`, from that stream's memory: memory of the current stream may still be
+    read there by work that was queued before it was freed."""
+    import torch
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(_on(stream, device)):
+        return torch.empty(shape, dtype=dtype, device=device)
 
 
 def _fail(rc, where):
@@ -220,8 +241,7 @@ def qtea_kv_append(cache: KVCache, batch: KVBatch, k, v, q=None, cos=None, sin=N
             raise ValueError(f"q has shape {tuple(q.shape)}, not whole heads of {dim}")
         qp, q_ld = _rows(q, dtype, "q", n, heads * dim)
         if q_out is None:
-            import torch
-            q_out = torch.empty((n, heads, dim), dtype=f16, device=q.device)
+            q_out = _new((n, heads, dim), f16, q.device, stream)
         op = _array(q_out, f16, "q_out", (n, heads, dim))
     cp = sp = positions = qn = kn = 0
     if cos is not None:
@@ -256,10 +276,9 @@ def qtea_kv_read(cache: KVCache, batch: KVBatch, row_start, n_rows=None, k_out=N
             raise ValueError("n_rows is needed to make the outputs")
         n_rows = (k_out if k_out is not None else v_out).shape[0]
     shape = (int(n_rows), cache.n_kv_heads, cache.head_dim)
-    if k_out is None and v_out is None:
-        import torch
-        k_out, v_out = (torch.empty(shape, dtype=torch.float16, device=cache.k_pages.device) for _ in range(2))
     f16 = _state["f16"]
+    if k_out is None and v_out is None:
+        k_out, v_out = (_new(shape, f16, cache.k_pages.device, stream) for _ in range(2))
     rc = lib.qtea_kv_read(cache.handle, batch._ref,
                           _array(row_start, _state["i32"], "row_start", (batch._c.n_seqs + 1,)), shape[0],
                           _array(k_out, f16, "k_out", shape) if k_out is not None else None,
@@ -289,8 +308,7 @@ def attention_workspace(device=None, stream=None):
     ws = _workspaces.get((device, raw))
     if ws is None:
         n = ctypes.c_size_t()
-        on = torch.cuda.ExternalStream(raw, device=device) if raw else torch.cuda.default_stream(device)
-        with torch.cuda.device(device), torch.cuda.stream(on):
+        with torch.cuda.device(device), torch.cuda.stream(_on(raw, device)):
             rc = lib.qtea_attention_workspace(ctypes.byref(n))
             if rc:
                 _fail(rc, "qtea_attention_workspace")
@@ -316,8 +334,7 @@ def qtea_attention(cache: KVCache, batch: KVBatch, q, scale=None, window: int = 
     heads = shape[1]
     q_ptr, q_ld = _rows(q, _state["f16"], "q", n, heads * dim)
     if out is None:
-        import torch
-        out = torch.empty((n, heads, dim), dtype=torch.float16, device=q.device)
+        out = _new((n, heads, dim), _state["f16"], q.device, stream)
     o_ptr, o_ld = _rows(out, _state["f16"], "out", n, heads * dim)
     stream = _stream_of(stream, cache.device)
     if workspace is None:
@@ -379,8 +396,7 @@ def qtea_norm(h, weight=None, y=None, post_weight=None, gate=None, res_scale: fl
             raise ValueError("x needs weight")
         wp = _array(weight, f16, "weight", (cols,))
         if x is None:
-            import torch
-            x = torch.empty((n, cols), dtype=f16, device=h.device)
+            x = _new((n, cols), f16, h.device, stream)
         xp, x_ld = _rows(x, f16, "x", n, cols)
     elif y is None:
         raise ValueError("nothing to do without y and x")

@@ -308,6 +308,42 @@ def test_attention_on_two_streams_with_their_own_workspaces(qt):
     assert all(torch.equal(a, b) for a, b in zip(outs, ref))
 
 
+@pytest.mark.parametrize("op", ["append", "read", "attention", "norm"])
+def test_outputs_on_another_stream_take_no_memory_in_use(qt, op):
+    """What the current stream has still to read, though freed, is not an output of a call on another."""
+    n = 12288  # 12 MB of fp16: a block of the allocator's own, taken again by what has its size
+    cache = qt.KVCache.empty(n // 64, 64, 4, 128)
+    i32 = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    batch = qt.KVBatch(i32([0, n]), i32([n]), i32([list(range(n // 64))]), n, n)
+    rows = torch.randn(n, 4 * 128, device="cuda").half()
+    weight, row_start = torch.ones(512, device="cuda").half(), i32([0, n])
+    s = torch.cuda.Stream()
+    calls = {"append": lambda **k: qt.qtea_kv_append(cache, batch, rows, rows, q=rows, stream=s,
+                                                     **({"q_out": k["out"][0]} if k else {})),
+             "read": lambda **k: qt.qtea_kv_read(cache, batch, row_start, n_rows=n, stream=s,
+                                                 **(dict(zip(("k_out", "v_out"), k["out"])) if k else {})),
+             "attention": lambda **k: qt.qtea_attention(cache, batch, rows.view(n, 4, 128), stream=s.cuda_stream,
+                                                        **({"out": k["out"][0]} if k else {})),
+             "norm": lambda **k: qt.qtea_norm(rows, weight, stream=s,
+                                              **({"x": k["out"][0].view(n, 512)} if k else {}))}
+    taken = [torch.empty(n, 4, 128, dtype=torch.float16, device="cuda") for _ in range(2)]
+    copies = [torch.empty_like(t) for t in taken]
+    calls["append"]()
+    calls[op](out=taken)  # the kernels are loaded
+    torch.cuda.synchronize()
+    torch.cuda.empty_cache()
+    for t in taken:
+        t.fill_(7)
+    torch.cuda.synchronize()
+    torch.cuda._sleep(50_000_000)
+    for t, copy in zip(taken, copies):
+        copy.copy_(t)
+    del t, taken
+    out = calls[op]()
+    torch.cuda.synchronize()
+    assert all(bool((copy == 7).all()) for copy in copies) and out is not None
+
+
 def test_offsets_past_32_bits(qt):
     """Pages more than 4 GB into the cache: written, read back and attended to as those at its start."""
     n_pages, heads, dim, page = 20000, 8, 128, 128  # 5.2 GB a side
