@@ -198,7 +198,7 @@ __global__ void __launch_bounds__(kWarps * 32, (Rows<FMT, D, NT>::kCtas))
     // it was issued.
     auto page_of = [&](int i) {
       const int key = ((it.unit0 + warp + kWarps * i) << T::kShift) + box * lane;
-      return __ldg(pages + min(key >> p.kv.page_shift, p.b.max_pages - 1));
+      return pages[min(key >> p.kv.page_shift, p.b.max_pages - 1)];
     };
     int next_page = lane < boxes && mine > 0 ? page_of(0) : 0;
     auto issue = [&](int i, uint32_t stage) {

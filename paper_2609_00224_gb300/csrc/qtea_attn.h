@@ -74,6 +74,8 @@ cudaError_t attn_launch(void (*kernel)(Params...), int grid, int threads, int sm
   cfg.numAttrs = 1;
   return cudaLaunchKernelEx(&cfg, kernel, args...);
 }
+// What earlier kernels wrote is read behind the wait, by ordinary loads: a read-only one (__ldg) may be moved ahead
+// of it, and what it reads may not change while the kernel, already launched, waits.
 __device__ __forceinline__ void attn_begin() {
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");
@@ -98,7 +100,7 @@ __device__ __forceinline__ AttnTable attn_table(void* memory, int n_seqs) {
 
 __device__ __forceinline__ AttnSeq attn_seq(const AttnParams& p, int s) {
   AttnSeq a;
-  const int q0 = __ldg(p.b.q_start + s), q1 = __ldg(p.b.q_start + s + 1), ctx = kv_context(p.b, p.kv, s);
+  const int q0 = p.b.q_start[s], q1 = p.b.q_start[s + 1], ctx = kv_context(p.b, p.kv, s);
   a.q0 = min(max(q0, 0), p.b.n_tokens);
   const int n = min(max(q1, a.q0), p.b.n_tokens) - a.q0;
   a.base = ctx - n;

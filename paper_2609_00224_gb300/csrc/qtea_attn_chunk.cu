@@ -357,7 +357,7 @@ __global__ void __launch_bounds__((Chunk<FMT, D>::kThreads), 1)
           int unit;
           bool value;
           order.at(i, &unit, &value);
-          return __ldg(pages + min((key_item + unit * kUnit) >> p.kv.page_shift, p.b.max_pages - 1));
+          return pages[min((key_item + unit * kUnit) >> p.kv.page_shift, p.b.max_pages - 1)];
         };
         int ahead[2] = {page_of(mine), page_of(mine + 2)};
         for (int i = mine; i < order.steps(); i += 2) {

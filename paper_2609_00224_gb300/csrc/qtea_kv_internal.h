@@ -42,7 +42,7 @@ int check_batch(const qtea_kv* kv, const qtea_kv_batch* b, bool queries, KvBatch
 // A sequence's context length as the kernels take it: within what its page table can name.
 __device__ __forceinline__ int kv_context(const KvBatchView& b, const KvView& kv, int s) {
   const int most = b.max_pages << kv.page_shift;  // < 2^31 (checked on the host)
-  return min(max(__ldg(b.ctx_len + s), 0), most);
+  return min(max(b.ctx_len[s], 0), most);
 }
 
 // The sequence whose rows [start[s], start[s+1]) hold `row`, found by one warp (all 32 lanes call it,
