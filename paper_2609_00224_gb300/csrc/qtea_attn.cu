@@ -153,7 +153,7 @@ __global__ void __launch_bounds__(kWarps * 32, (Rows<FMT, D, NT>::kCtas))
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   const AttnTable tab = attn_table(smem + T::kRing + T::kScaleRing, p.b.n_seqs);
-  attn_begin();
+  pdl_begin();
   attn_prefix(p, tab);
   int cur;
   {

@@ -10,6 +10,7 @@
 #pragma once
 
 #include "qtea_kv_internal.h"
+#include "qtea_pdl.h"
 
 namespace qtea {
 
@@ -55,30 +56,11 @@ inline bool attn_cost_fits(const AttnParams& p) {
 
 #ifdef __CUDACC__
 
-// Launch with programmatic stream serialization: the grid may start while the kernel before it on the
-// stream drains, and waits for it (attn_begin) before it touches the caller's memory.
 template <class... Params, class... Args>
 cudaError_t attn_launch(void (*kernel)(Params...), int grid, int threads, int smem, cudaStream_t st,
                         const Args&... args) {
   cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
-  if (e != cudaSuccess) return e;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(grid);
-  cfg.blockDim = dim3(threads);
-  cfg.dynamicSmemBytes = smem;
-  cfg.stream = st;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, kernel, args...);
-}
-// What earlier kernels wrote is read behind the wait, by ordinary loads: a read-only one (__ldg) may be moved ahead
-// of it, and what it reads may not change while the kernel, already launched, waits.
-__device__ __forceinline__ void attn_begin() {
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-  asm volatile("griddepcontrol.wait;" ::: "memory");
+  return e != cudaSuccess ? e : pdl_launch(kernel, grid, threads, smem, st, args...);
 }
 
 // One sequence of the batch.

@@ -318,7 +318,7 @@ __global__ void __launch_bounds__((Chunk<FMT, D>::kThreads), 1)
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   const AttnTable tab = attn_table(smem_raw + T::kSmem, p.b.n_seqs);
-  attn_begin();
+  pdl_begin();
   attn_prefix(p, tab);  // ends with a barrier
   const AttnSplit split = attn_split(p, tab);
   if (split.total == 0 || (int)blockIdx.x >= split.ctas) return;

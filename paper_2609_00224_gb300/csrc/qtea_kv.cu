@@ -8,6 +8,7 @@
 #include <new>
 
 #include "qtea_kv_internal.h"
+#include "qtea_pdl.h"
 
 namespace qtea {
 namespace {
@@ -60,11 +61,11 @@ __device__ __forceinline__ void load4(const char* p, float* v) {
 template <bool VEC>
 __device__ __forceinline__ void table4(const float* p, float* v) {
   if (VEC) {
-    const float4 x = __ldg(reinterpret_cast<const float4*>(p));
+    const float4 x = *reinterpret_cast<const float4*>(p);
     v[0] = x.x, v[1] = x.y, v[2] = x.z, v[3] = x.w;
   } else {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = __ldg(p + e);
+    for (int e = 0; e < 4; ++e) v[e] = p[e];
   }
 }
 
@@ -81,12 +82,13 @@ __device__ __forceinline__ float saturate_f16(float x) {  // NaN stays NaN
 // with the elements 4l.. of the head's first half and of its second, the two that a rotation joins.
 // 8 lanes hold a block of 32 elements of either half, whatever D is. All passes' loads are issued
 // before the first is used: 4 KB a warp at fp32, which is what keeps memory busy.
-// 8192 tokens of 32 + 8 + 8 heads from fp32 to fp16 on GB300: 306 MB in 52 us (one head a warp, with
+// 8192 tokens of 32 + 8 + 8 heads from fp32 to fp16 on GB300: 306 MB in 54 us (one head a warp, with
 // 4-byte accesses, took 88 us).
 template <int TYPE, int FMT, int D, bool VEC>
 __global__ void __launch_bounds__(kAppendWarps * 32) qtea_kv_append_kernel(const AppendParams p) {
   constexpr int kLanes = D / 8, kPerPass = 32 / kLanes, kPerWarp = kAppendPasses * kPerPass;
   constexpr int kSize = TYPE == QTEA_TYPE_F32 ? 4 : 2;
+  pdl_begin();
   const int lane = threadIdx.x & 31, l = lane % kLanes, heads = p.q_heads + 2 * p.kv.heads;
   const int warps = (heads + kPerWarp - 1) / kPerWarp;  // of a token
   const long long job = (long long)blockIdx.x * kAppendWarps + (threadIdx.x >> 5);
@@ -111,7 +113,7 @@ __global__ void __launch_bounds__(kAppendWarps * 32) qtea_kv_append_kernel(const
   if (f.s < 0 || t - f.first >= p.b.max_q) return;
   const int pos = f.ctx - min(f.next, p.b.n_tokens) + t;
   int page = -1;
-  if (pos >= 0) page = __ldg(p.b.pages + (long long)f.s * p.b.max_pages + (pos >> p.kv.page_shift));
+  if (pos >= 0) page = p.b.pages[(long long)f.s * p.b.max_pages + (pos >> p.kv.page_shift)];
   const bool stored = (unsigned)page < (unsigned)p.kv.n_pages;
   float c[4], d[4];
   if (p.cos) {
@@ -221,11 +223,12 @@ constexpr int kReadRows = 16;  // output rows of a CTA, at most
 // A CTA takes a few consecutive output rows: its warps find the rows' places in the cache, a row at a
 // time (the sequence from row_start, 32 sequences a load, with their lengths beside them), then
 // every thread converts 16 elements at a time, so that a warp's stores are one run of memory. 16
-// elements are 32, 16 or 8 bytes of codes, one load each. 100003 tokens of 8 heads (fp8), 621 MB, take 101 us on
-// GB300 (6.1 TB/s, two thirds of it written).
+// elements are 32, 16 or 8 bytes of codes, one load each. 100003 tokens of 8 heads (fp8), 621 MB, take 100 us on
+// GB300 (6.2 TB/s, two thirds of it written).
 template <int FMT, int D>
 __global__ void __launch_bounds__(kReadThreads) qtea_kv_read_kernel(const ReadParams p) {
   __shared__ long long where[kReadRows];  // slot of head 0, -1: zeros, -2: no sequence's row
+  pdl_begin();
   const int r0 = blockIdx.x * p.rows, lane = threadIdx.x & 31;
   for (int i = threadIdx.x >> 5; i < p.rows; i += kReadThreads / 32) {
     const int r = r0 + i;
@@ -235,7 +238,7 @@ __global__ void __launch_bounds__(kReadThreads) qtea_kv_read_kernel(const ReadPa
       const int pos = r - f.first;
       if (f.s >= 0) at = -1;
       if (f.s >= 0 && pos < f.ctx) {
-        const int page = __ldg(p.b.pages + (long long)f.s * p.b.max_pages + (pos >> p.kv.page_shift));
+        const int page = p.b.pages[(long long)f.s * p.b.max_pages + (pos >> p.kv.page_shift)];
         if ((unsigned)page < (unsigned)p.kv.n_pages)
           at = (long long)page * p.kv.heads * p.kv.page_size + (pos & (p.kv.page_size - 1));
       }
@@ -267,7 +270,7 @@ __global__ void __launch_bounds__(kReadThreads) qtea_kv_read_kernel(const ReadPa
           o[0] = x.x, o[1] = x.y, o[2] = x.z, o[3] = x.w, o[4] = y.x, o[5] = y.y, o[6] = y.z, o[7] = y.w;
         } else {
           const uint8_t* scales = side == 0 ? p.kv.ks : p.kv.vs;
-          const uint32_t f = scale_bits(__ldg(scales + slot * (D / kKvBlock) + c / 2)) * 0x10001u;
+          const uint32_t f = scale_bits(scales[slot * (D / kKvBlock) + c / 2]) * 0x10001u;
           if (FMT == QTEA_KV_FP8) {
             const uint4 x = __ldcs(reinterpret_cast<const uint4*>(src));
             const uint32_t v[4] = {x.x, x.y, x.z, x.w};
@@ -297,18 +300,18 @@ void launch_append(const AppendParams& p, bool vec, cudaStream_t st) {
   const long long jobs = (long long)p.b.n_tokens * ((heads + per_warp - 1) / per_warp);
   const unsigned grid = (unsigned)((jobs + kAppendWarps - 1) / kAppendWarps);  // < 2^31 (checked)
   if (p.kv.dim == 128) {
-    if (vec) qtea_kv_append_kernel<TYPE, FMT, 128, true><<<grid, kAppendWarps * 32, 0, st>>>(p);
-    else qtea_kv_append_kernel<TYPE, FMT, 128, false><<<grid, kAppendWarps * 32, 0, st>>>(p);
+    if (vec) pdl_launch(qtea_kv_append_kernel<TYPE, FMT, 128, true>, grid, kAppendWarps * 32, 0, st, p);
+    else pdl_launch(qtea_kv_append_kernel<TYPE, FMT, 128, false>, grid, kAppendWarps * 32, 0, st, p);
   } else {
-    if (vec) qtea_kv_append_kernel<TYPE, FMT, 64, true><<<grid, kAppendWarps * 32, 0, st>>>(p);
-    else qtea_kv_append_kernel<TYPE, FMT, 64, false><<<grid, kAppendWarps * 32, 0, st>>>(p);
+    if (vec) pdl_launch(qtea_kv_append_kernel<TYPE, FMT, 64, true>, grid, kAppendWarps * 32, 0, st, p);
+    else pdl_launch(qtea_kv_append_kernel<TYPE, FMT, 64, false>, grid, kAppendWarps * 32, 0, st, p);
   }
 }
 
 template <int FMT>
 void launch_read(const ReadParams& p, int grid, cudaStream_t st) {
-  if (p.kv.dim == 128) qtea_kv_read_kernel<FMT, 128><<<grid, kReadThreads, 0, st>>>(p);
-  else qtea_kv_read_kernel<FMT, 64><<<grid, kReadThreads, 0, st>>>(p);
+  if (p.kv.dim == 128) pdl_launch(qtea_kv_read_kernel<FMT, 128>, grid, kReadThreads, 0, st, p);
+  else pdl_launch(qtea_kv_read_kernel<FMT, 64>, grid, kReadThreads, 0, st, p);
 }
 
 }  // namespace
@@ -351,7 +354,8 @@ int qtea_kv_create(void* k_pages, void* v_pages, void* k_scales, void* v_scales,
   cudaDriverEntryPointQueryResult found;
   if (cudaGetDevice(&dev) != cudaSuccess ||
       cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess ||
-      cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000, cudaEnableDefault, &found) != cudaSuccess ||
+      cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000, cudaEnableDefault, &found) !=
+          cudaSuccess ||
       found != cudaDriverEntryPointSuccess) {
     cudaGetLastError();
     return QTEA_ERR_CUDA;

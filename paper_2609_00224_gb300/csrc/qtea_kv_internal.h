@@ -59,7 +59,7 @@ __device__ __forceinline__ KvFound kv_find_sequence(const int32_t* start, const 
     const int s = base + lane;
     int first = 0, next = 0, ctx = 0;
     if (s < b.n_seqs) {
-      first = __ldg(start + s), next = __ldg(start + s + 1);
+      first = start[s], next = start[s + 1];
       ctx = kv_context(b, kv, s);
     }
     const unsigned m = __ballot_sync(0xffffffffu, row >= first && row < next);

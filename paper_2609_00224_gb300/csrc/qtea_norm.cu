@@ -10,6 +10,7 @@
 #include <algorithm>
 
 #include "qtea_internal.h"
+#include "qtea_pdl.h"
 
 namespace qtea {
 namespace {
@@ -138,6 +139,7 @@ __device__ __forceinline__ float cta_sum(float v, float* part) {
 template <int HT, int YT, int C, bool VEC>
 __global__ void __launch_bounds__(C == 1 ? 1024 : 512, C == 1 && VEC ? 2 : 1) qtea_norm_kernel(const NormParams p) {
   __shared__ float part[2][32];
+  pdl_begin();
   const int n = p.n;
   const float inv_n = 1.f / (float)n;
   for (int r = blockIdx.x; r < p.n_rows; r += gridDim.x) {
@@ -206,6 +208,7 @@ __global__ void __launch_bounds__(C == 1 ? 1024 : 512, C == 1 && VEC ? 2 : 1) qt
 template <int HT, int YT>
 __global__ void __launch_bounds__(1024) qtea_norm_long_kernel(const NormParams p) {
   __shared__ float part[2][32];
+  pdl_begin();
   const float inv_n = 1.f / (float)p.n;
   for (int r = blockIdx.x; r < p.n_rows; r += gridDim.x) {
     const void* hrow = at(p.h, r, p.h_ld, HT);
@@ -259,13 +262,13 @@ void launch_types(const NormParams& p, bool vec, cudaStream_t st) {
   const bool wide = per8 > 1024;  // more than a chunk for each of the most threads
   const int threads = std::max(32, (((wide ? (per8 + 3) / 4 : per8) + 31) / 32) * 32);
   if (wide && (!vec || per8 > 4 * 512)) {
-    qtea_norm_long_kernel<HT, YT><<<grid, 1024, 0, st>>>(p);
+    pdl_launch(qtea_norm_long_kernel<HT, YT>, grid, 1024, 0, st, p);
   } else if (wide) {
-    qtea_norm_kernel<HT, YT, 4, true><<<grid, threads, 0, st>>>(p);
+    pdl_launch(qtea_norm_kernel<HT, YT, 4, true>, grid, threads, 0, st, p);
   } else if (vec) {
-    qtea_norm_kernel<HT, YT, 1, true><<<grid, threads, 0, st>>>(p);
+    pdl_launch(qtea_norm_kernel<HT, YT, 1, true>, grid, threads, 0, st, p);
   } else {
-    qtea_norm_kernel<HT, YT, 1, false><<<grid, threads, 0, st>>>(p);
+    pdl_launch(qtea_norm_kernel<HT, YT, 1, false>, grid, threads, 0, st, p);
   }
 }
 
